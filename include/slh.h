@@ -51,6 +51,7 @@ typedef struct slh_ctx slh_ctx;
 /* element types of X */
 #define SLH_BF16 0        /* bfloat16, raw 16-bit patterns                          */
 #define SLH_F32  1        /* float32                                                */
+#define SLH_F16  2        /* float16, raw patterns: the attention operators only    */
 
 /* options for slh_set_option (set before slh_feature_map) */
 #define SLH_OPT_KERNEL        1  /* 0: unbiased for exp(x.y/sqrt(D)) (default): the
@@ -453,6 +454,117 @@ int slh_peak_mfma(int32_t reps, void *sink, void *stream, double *tflops_out);
 int slh_merge_noalloc(const void *X, int32_t x_dtype, int64_t ldx, int64_t N, int64_t D,
                       const uint32_t *codes, int32_t bits, float *emb_out, int32_t *pos_out,
                       int32_t *tok2macro_out, int64_t cap, int64_t *M_out, void *stream);
+
+/*
+ * The operators behind a compressed prompt: what an LLM's attention layers do with the
+ * macro-tokens.  They need no context and keep nothing between calls: every pointer is device
+ * memory of the caller, the work goes to `stream` (a hipStream_t, NULL = null stream) and no call
+ * waits for it, so each may be captured into a graph.  SLH_EINVAL before any GPU work for
+ * what the host can see (sizes, strides, alignment, pointers); what lies in device memory
+ * (positions, slots, lengths, page entries) cannot be refused by the host and is kept in
+ * bounds by the kernels as each call states.
+ *
+ * Rows: element (token t, head h, e) of a tensor lies at t st + h sh + e, for strides st and sh
+ * in elements.  Pointers are aligned to 16 bytes and strides are multiples of 8 and not negative,
+ * so queries, keys and values may be parts of one projection's rows.  Outputs must not
+ * overlap inputs, unless a call says so.
+ */
+
+/*
+ * The table of cosines and sines that the rotations read: table[p][0][i] = s cos(p f_i),
+ * table[p][1][i] = s sin(p f_i) for positions 0 <= p < n_pos and i < rot_dim / 2, evaluated in
+ * 64 bits and stored in 32 (device, n_pos rot_dim floats).  f_i = base^(-2 i / rot_dim) and
+ * s = 1, for contexts longer than the `orig_len` tokens of the training:
+ *   SLH_ROPE_LINEAR  f_i / factor (positions interpolated)
+ *   SLH_ROPE_BASE    base factor^(rot_dim / (rot_dim - 2)) in the place of base
+ *   SLH_ROPE_BANDS   f_i where it turns beta_fast times or more within orig_len tokens, f_i / factor
+ *                    where beta_slow times or fewer, in between mixed linearly in the turns;
+ *                    s = 0.1 ln(factor) + 1
+ * rot_dim: a multiple of 16 from 16 to 256; base > 1; factor >= 1; 0 < beta_slow < beta_fast.
+ */
+#define SLH_ROPE_PLAIN  0
+#define SLH_ROPE_LINEAR 1
+#define SLH_ROPE_BASE   2
+#define SLH_ROPE_BANDS  3
+int slh_rope_table(float *table, int64_t n_pos, int32_t rot_dim, double base, int32_t scaling,
+                   double factor, int64_t orig_len, double beta_fast, double beta_slow,
+                   void *stream);
+
+/*
+ * Norms of queries and keys for each head, and the rotation, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) w          (where weights are given: d elements of `dtype`)
+ *   (a, b) -> (a cos - b sin, b cos + a sin) over the first rot_dim elements (table not NULL):
+ *     pairs (i, i + rot_dim / 2), or (2 i, 2 i + 1) where `interleaved`
+ * in fp32 with one rounding to dtype (SLH_BF16, SLH_F16, SLH_F32).  pos: T positions; the rotated
+ * elements of a token whose position lies outside [0, n_pos) become NaN.  Hq or Hk may be 0
+ * (its pointers are then not used).  Outputs may be their inputs (same pointer and strides).
+ * d: a multiple of 8 from 8 to 256; rot_dim as for the table, at most d, and 0 without one.
+ * T (Hq + Hk) < 2^27.
+ */
+int slh_qk_norm_rope(const void *q, int64_t q_st, int64_t q_sh, int32_t Hq, void *q_out,
+                     int64_t qo_st, int64_t qo_sh, const void *k, int64_t k_st, int64_t k_sh,
+                     int32_t Hk, void *k_out, int64_t ko_st, int64_t ko_sh, int32_t dtype,
+                     int64_t T, int32_t d, const void *q_weight, const void *k_weight, double eps,
+                     const float *table, int64_t n_pos, int32_t rot_dim, const int32_t *pos,
+                     int32_t interleaved, void *stream);
+
+/*
+ * New keys and values into a paged cache, the keys normed and rotated on the way (as above; NULL
+ * weights and a NULL table leave them as they are).  k_cache, v_cache: [n_pages][H][page_size][d],
+ * page_size a power of two up to 65536.  Token t goes to row slots[t] % page_size of page
+ * slots[t] / page_size; a token whose slot lies outside [0, n_pages page_size) is left out
+ * (-1: padding).  Two tokens with one slot: either may win, element by element.
+ */
+int slh_kv_append(const void *k, int64_t k_st, int64_t k_sh, const void *v, int64_t v_st,
+                  int64_t v_sh, int32_t dtype, int64_t T, int32_t H, int32_t d,
+                  const void *k_weight, double eps, const float *table, int64_t n_pos,
+                  int32_t rot_dim, const int32_t *pos, int32_t interleaved, void *k_cache,
+                  void *v_cache, int64_t n_pages, int32_t page_size, const int64_t *slots,
+                  void *stream);
+
+/*
+ * Attention over packed prompts of different lengths.  Sequence b has the queries
+ * cu_q[b] <= t < cu_q[b + 1] of q and the keys cu_k[b] <= t < cu_k[b + 1] of k and v (device, B + 1
+ * entries each, ascending; entries outside [0, Tq] or [0, Tk] are taken as the nearest of these).
+ *   out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i . k_j),  j < limit_i
+ * limit_i = the sequence's keys, or, where `causal`, keys - queries + i + 1: the last query sees
+ * every key, so keys of a cached context may stand before the queries' own.  A query that sees
+ * no key gets zeros.  What a query does not see does not reach it, infinities and NaN included.
+ * Query head h reads key/value head h / (Hq / Hkv).  dtype: SLH_BF16 or SLH_F16; d: 64, 80, 96 or
+ * 128.  Products of dtype with fp32 accumulation, softmax in fp32; the weights are rounded to dtype
+ * for the second product.  lse: [Tq][Hq] floats, ln sum_j p_ij (-inf where nothing is seen), or NULL.
+ * workspace: slh_attend_workspace() bytes of device memory (aligned to 16 bytes, contents need no
+ * preparation), which no other call may use until this one has run; the size is for the current
+ * device.  Rows of out that belong to no sequence are not written.
+ */
+int64_t slh_attend_workspace(int64_t Tq, int64_t Tk, int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
+int slh_attend(const void *q, int64_t q_st, int64_t q_sh, const void *k, int64_t k_st, int64_t k_sh,
+               const void *v, int64_t v_st, int64_t v_sh, int32_t dtype, int64_t Tq, int64_t Tk,
+               int32_t B, int32_t Hq, int32_t Hkv, int32_t d, const int32_t *cu_q,
+               const int32_t *cu_k, double scale, int32_t causal, void *out, int64_t o_st,
+               int64_t o_sh, float *lse, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * The new tokens of a batch against a paged cache (as slh_kv_append writes it), behind a prefix that
+ * every sequence shares: a decode step, or a few tokens at once.  Tokens b n_q <= t < (b + 1) n_q of
+ * q and out are sequence b's.  Its keys are the prefix_len rows of prefix_pages (ceil(prefix_len /
+ * page_size) entries; read once for all sequences) and lens[b] rows of its own pages, page_table[b
+ * ld_pages + i] (max_pages entries), the n_q new tokens' own last among them: token i sees the
+ * prefix and the first lens[b] - n_q + i + 1 own rows.  prefix_len 0: no prefix.  lens outside
+ * [0, max_pages page_size] are taken as the nearest of these; results of a sequence whose pages
+ * lie outside [0, n_pages) are undefined, but nothing outside the cache is read.  Types, heads,
+ * products, lse ([B n_q][Hq]) and workspace (slh_attend_paged_workspace(), with max_len =
+ * max_pages page_size) as for slh_attend.
+ */
+int64_t slh_attend_paged_workspace(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d,
+                                   int64_t max_len, int64_t prefix_len);
+int slh_attend_paged(const void *q, int64_t q_st, int64_t q_sh, const void *k_cache,
+                     const void *v_cache, int32_t dtype, int64_t n_pages, int32_t page_size,
+                     int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d,
+                     const int32_t *page_table, int64_t ld_pages, int32_t max_pages,
+                     const int32_t *lens, const int32_t *prefix_pages, int64_t prefix_len,
+                     double scale, void *out, int64_t o_st, int64_t o_sh, float *lse,
+                     void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Number of windows and of spectral windows of the current routing. */
 int64_t slh_num_windows(const slh_ctx *ctx);

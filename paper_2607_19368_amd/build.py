@@ -32,6 +32,8 @@ SOURCES = [
     "k_route.hip",
     "k_peak.hip",
     "slh_noalloc.hip",
+    "k_rope.hip",
+    "k_attend.hip",
 ]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -15,7 +15,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libslh.so")
 
 SLH_OK, SLH_EINVAL, SLH_ENOMEM, SLH_EHIP, SLH_ESTATE = 0, -1, -2, -3, -4
-SLH_BF16, SLH_F32 = 0, 1
+SLH_BF16, SLH_F32, SLH_F16 = 0, 1, 2
+SLH_ROPE_PLAIN, SLH_ROPE_LINEAR, SLH_ROPE_BASE, SLH_ROPE_BANDS = 0, 1, 2, 3
 SLH_OPT_KERNEL, SLH_OPT_WINDOW_LEN, SLH_OPT_POS_MODE, SLH_OPT_BREAKDOWN_TOL, SLH_OPT_TIMING = 1, 2, 3, 4, 5
 SLH_OPT_SHORT_WINDOWS, SLH_OPT_NORMALIZE, SLH_OPT_POS_SCHEME, SLH_OPT_KEEP_LAST = 6, 7, 8, 9
 SLH_OPT_TARGET_LEN, SLH_OPT_RESIDENT, SLH_OPT_WAIT_POLLS, SLH_OPT_DISTINCT = 10, 11, 12, 13
@@ -31,6 +32,8 @@ EXPORTS = [
     "slh_num_spectral", "slh_load", "slh_stage_times", "slh_time_passes", "slh_spectral_energy",
     "slh_bucket_purity", "slh_eigh_ritz", "slh_peak_read", "slh_peak_mfma", "slh_merge_noalloc",
     "slh_merge_async", "slh_merge_wait", "slh_operator_rows",
+    "slh_rope_table", "slh_qk_norm_rope", "slh_kv_append", "slh_attend_workspace", "slh_attend",
+    "slh_attend_paged_workspace", "slh_attend_paged",
 ]
 
 _lib = None
@@ -49,6 +52,7 @@ def load():
         raise SLHError(f"{LIB_PATH} is not built; run `python -m paper_2607_19368_amd.build`")
     L = ctypes.CDLL(LIB_PATH)
     vp, i32, i64, u64, dp = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_void_p
+    f64 = ctypes.c_double
     sig = {
         "slh_gen_params": (i32, [u64, i64, i64, i32, i32, vp, vp, vp]),
         "slh_gen_start": (i32, [u64, i64, i64, vp]),
@@ -78,6 +82,17 @@ def load():
         "slh_bucket_purity": (i32, [vp, vp, i32, i64, ctypes.c_double, vp]),
         "slh_stage_times": (i32, [vp, vp, i32]),
         "slh_time_passes": (i32, [vp, i32, vp]),
+        "slh_rope_table": (i32, [vp, i64, i32, f64, i32, f64, i64, f64, f64, vp]),
+        "slh_qk_norm_rope": (i32, [vp, i64, i64, i32, vp, i64, i64] * 2
+                             + [i32, i64, i32, vp, vp, f64, vp, i64, i32, vp, i32, vp]),
+        "slh_kv_append": (i32, [vp, i64, i64, vp, i64, i64, i32, i64, i32, i32, vp, f64, vp, i64, i32, vp, i32,
+                                vp, vp, i64, i32, vp, vp]),
+        "slh_attend_workspace": (i64, [i64, i64, i32, i32, i32, i32]),
+        "slh_attend": (i32, [vp, i64, i64] * 3 + [i32, i64, i64, i32, i32, i32, i32, vp, vp, f64, i32, vp, i64, i64,
+                                                  vp, vp, i64, vp]),
+        "slh_attend_paged_workspace": (i64, [i32, i32, i32, i32, i32, i64, i64]),
+        "slh_attend_paged": (i32, [vp, i64, i64, vp, vp, i32, i64, i32, i32, i32, i32, i32, i32, vp, i64, i32, vp,
+                                   vp, i64, f64, vp, i64, i64, vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
