@@ -13,59 +13,76 @@ _DTYPES = {torch.bfloat16: B.SLH_BF16, torch.float16: B.SLH_F16, torch.float32: 
 _HALVES = (torch.bfloat16, torch.float16)
 
 
-def _fail(what, rc):
-    raise SLHError(f"{what} failed ({rc}): " + {
-        B.SLH_EINVAL: "a size, stride or alignment that the library does not take",
-        B.SLH_EHIP: "a kernel launch failed"}.get(rc, ""))
+# The calls of a decode step take microseconds, so the checks here are few and flat: dtypes are
+# singletons, devices are compared by index, and the stream is asked for as an integer.
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _stream(stream, device):
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+def _call(name, dev, stream, args):
+    """Calls the library's function `name` on device `dev` with args and the stream."""
+    f = getattr(B.load(), name)
+    if torch.cuda.current_device() == dev:
+        rc = f(*args, _current_stream(dev) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = f(*args, _current_stream(dev) if stream is None else stream.cuda_stream)
+    if rc != B.SLH_OK:
+        raise SLHError(f"{name} failed ({rc}): " + {
+            B.SLH_EINVAL: "a size, stride or alignment that the library does not take",
+            B.SLH_EHIP: "a kernel launch failed"}.get(rc, ""))
 
 
-def _rows(name, t, dims=3, like=None, shape=None):
-    """t: a device tensor of rows ([token, head, element] at its end) with unit element stride; of
-    the type and device of `like` and of `shape`, where given."""
+def _first(name, t, dims):
+    """(type, device index, shape, strides) of the tensor of rows that the others go by."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise SLHError(f"{name} must be a device tensor")
-    if t.dim() != dims or (t.stride(-1) != 1 and t.numel() > 0):
-        raise SLHError(f"{name} must have {dims} dimensions and unit stride in the last")
     if t.dtype not in _DTYPES:
         raise SLHError(f"{name}: unsupported type {t.dtype}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise SLHError(f"{name} must be {like.dtype} on {like.device}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    shape, st = t.shape, t.stride()
+    if len(shape) not in dims or (st[-1] != 1 and t.numel() > 0):
+        raise SLHError(f"{name} must have {' or '.join(map(str, dims))} dimensions and unit stride in the last")
+    return t.dtype, t.get_device(), shape, st
+
+
+def _rows(name, t, dtype, dev, shape):
+    """Strides of t, a tensor of rows with unit element stride."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev:
+        raise SLHError(f"{name} must be a {dtype} tensor on device {dev}")
+    if t.shape != shape:
         raise SLHError(f"{name} must have shape {tuple(shape)}")
+    st = t.stride()
+    if st[-1] != 1 and t.numel() > 0:
+        raise SLHError(f"{name} must have unit stride in the last dimension")
+    return st
 
 
-def _plain(name, t, dtype, device, shape):
-    """t: a contiguous device tensor of `dtype` and `shape` (None: any length)."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise SLHError(f"{name} must be a contiguous {dtype} tensor on {device}")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+def _plain(name, t, dtype, dev, shape):
+    """Address of t, a contiguous tensor of `shape` (an entry None: any length)."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise SLHError(f"{name} must be a contiguous {dtype} tensor on device {dev}")
+    have = t.shape
+    if have != shape and (len(have) != len(shape) or any(n is not None and n != m for n, m in zip(shape, have))):
         raise SLHError(f"{name} must have shape ({', '.join('*' if n is None else str(n) for n in shape)})")
+    return t.data_ptr()
 
 
-def _rotation(table, pos, T, device):
-    """(table pointer, n_pos, rot_dim, pos pointer) of a rotation, or of none."""
+def _empty(shape, dtype, dev, stream):
+    """Memory of the stream that the call goes to."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _rotation(table, pos, T, dev):
+    """(table address, n_pos, rot_dim, pos address) of a rotation, or of none."""
     if table is None:
         return None, 0, 0, None
-    _plain("table", table, torch.float32, device, (None, 2, None))
+    t = _plain("table", table, torch.float32, dev, (None, 2, None))
     if pos is None:
         raise SLHError("pos must be given with a table")
-    _plain("pos", pos, torch.int32, device, (T,))
-    return table.data_ptr(), table.shape[0], 2 * table.shape[2], pos.data_ptr()
-
-
-def _weight(name, w, x):
-    if w is None:
-        return None
-    _plain(name, w, x.dtype, x.device, (x.shape[-1],))
-    return w.data_ptr()
-
-
-def _address(t):
-    return None if t is None else t.data_ptr()
+    return t, table.shape[0], 2 * table.shape[2], _plain("pos", pos, torch.int32, dev, (T,))
 
 
 def slh_rope_table(n_pos, rot_dim, base=10000.0, scaling=B.SLH_ROPE_PLAIN, factor=1.0, orig_len=0,
@@ -74,12 +91,10 @@ def slh_rope_table(n_pos, rot_dim, base=10000.0, scaling=B.SLH_ROPE_PLAIN, facto
     slh_kv_append; `scaling` is one of SLH_ROPE_PLAIN, _LINEAR, _BASE and _BANDS."""
     if n_pos < 1 or rot_dim < 16 or rot_dim > 256 or rot_dim % 16:
         raise SLHError("n_pos must be positive and rot_dim a multiple of 16 from 16 to 256")
-    table = torch.empty((n_pos, 2, rot_dim // 2), dtype=torch.float32, device=device)
-    with torch.cuda.device(table.device):
-        rc = B.load().slh_rope_table(table.data_ptr(), n_pos, rot_dim, float(base), int(scaling), float(factor),
-                                     int(orig_len), float(beta_fast), float(beta_slow), _stream(stream, table.device))
-    if rc != B.SLH_OK:
-        _fail("slh_rope_table", rc)
+    table = _empty((n_pos, 2, rot_dim // 2), torch.float32, device, stream)
+    _call("slh_rope_table", table.get_device(), stream,
+          (table.data_ptr(), n_pos, rot_dim, float(base), int(scaling), float(factor), int(orig_len),
+           float(beta_fast), float(beta_slow)))
     return table
 
 
@@ -88,37 +103,30 @@ def slh_qk_norm_rope(q, k=None, q_weight=None, k_weight=None, eps=1e-6, table=No
     """Queries [T, Hq, d] and keys [T, Hk, d] (either may be None): RMS norm per head where a
     weight [d] is given, rotation by the table's rows `pos` [T] int32 where a table is.  Returns
     (q_out, k_out), which may be the inputs themselves."""
-    x = q if q is not None else k
-    if x is None:
-        raise SLHError("q or k must be given")
-    args = []
-    shape = None
-    outs = []
-    for name, t, out in (("q", q, q_out), ("k", k, k_out)):
-        if t is None:
-            args += (None, 0, 0, 0, None, 0, 0)
-            outs.append(None)
-            continue
-        _rows(name, t, 3, x)
-        if shape is not None and (t.shape[0], t.shape[2]) != shape:
+    dtype, dev, shape, st = _first("q" if q is not None else "k", q if q is not None else k, (3,))
+    T, _, d = shape
+    none = (None, 0, 0, 0, None, 0, 0)
+    qa = ka = none
+    if q is not None:
+        if q_out is None:
+            q_out = _empty(shape, dtype, q.device, stream)
+        so = _rows("q_out", q_out, dtype, dev, shape)
+        qa = (q.data_ptr(), st[0], st[1], shape[1], q_out.data_ptr(), so[0], so[1])
+    if k is not None:
+        shape = k.shape
+        if len(shape) != 3 or shape[0] != T or shape[2] != d:
             raise SLHError("q and k must have the same tokens and head size")
-        shape = (t.shape[0], t.shape[2])
-        if out is None:
-            out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        else:
-            _rows(name + "_out", out, 3, t, t.shape)
-        args += (t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], out.data_ptr(), out.stride(0), out.stride(1))
-        outs.append(out)
-    T, d = shape
-    tab, n_pos, rot, p = _rotation(table, pos, T, x.device)
-    wq = _weight("q_weight", q_weight, x)
-    wk = _weight("k_weight", k_weight, x)
-    with torch.cuda.device(x.device):
-        rc = B.load().slh_qk_norm_rope(*args, _DTYPES[x.dtype], T, d, wq, wk, float(eps), tab, n_pos, rot, p,
-                                       int(interleaved), _stream(stream, x.device))
-    if rc != B.SLH_OK:
-        _fail("slh_qk_norm_rope", rc)
-    return tuple(outs)
+        st = _rows("k", k, dtype, dev, shape)
+        if k_out is None:
+            k_out = _empty(shape, dtype, k.device, stream)
+        so = _rows("k_out", k_out, dtype, dev, shape)
+        ka = (k.data_ptr(), st[0], st[1], shape[1], k_out.data_ptr(), so[0], so[1])
+    tab, n_pos, rot, p = _rotation(table, pos, T, dev)
+    wq = None if q_weight is None else _plain("q_weight", q_weight, dtype, dev, (d,))
+    wk = None if k_weight is None else _plain("k_weight", k_weight, dtype, dev, (d,))
+    _call("slh_qk_norm_rope", dev, stream,
+          (*qa, *ka, _DTYPES[dtype], T, d, wq, wk, eps, tab, n_pos, rot, p, interleaved))
+    return (q_out if q is not None else None), (k_out if k is not None else None)
 
 
 def slh_kv_append(k, v, k_cache, v_cache, slots, k_weight=None, eps=1e-6, table=None, pos=None, interleaved=False,
@@ -126,37 +134,41 @@ def slh_kv_append(k, v, k_cache, v_cache, slots, k_weight=None, eps=1e-6, table=
     """Writes k and v [T, H, d] into the caches [pages, H, page, d] at rows `slots` [T] int64
     (page * page size + row; negative: left out), the keys normed and rotated on the way as
     in slh_qk_norm_rope.  Returns the caches."""
-    _rows("k", k)
-    _rows("v", v, 3, k, k.shape)
-    T, H, d = k.shape
-    _plain("k_cache", k_cache, k.dtype, k.device, (None, H, None, d))
-    _plain("v_cache", v_cache, k.dtype, k.device, k_cache.shape)
-    _plain("slots", slots, torch.int64, k.device, (T,))
-    tab, n_pos, rot, p = _rotation(table, pos, T, k.device)
-    wk = _weight("k_weight", k_weight, k)
-    with torch.cuda.device(k.device):
-        rc = B.load().slh_kv_append(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
-                                    _DTYPES[k.dtype], T, H, d, wk, float(eps), tab, n_pos, rot, p, int(interleaved),
-                                    k_cache.data_ptr(), v_cache.data_ptr(), k_cache.shape[0], k_cache.shape[2],
-                                    slots.data_ptr(), _stream(stream, k.device))
-    if rc != B.SLH_OK:
-        _fail("slh_kv_append", rc)
+    dtype, dev, shape, ks = _first("k", k, (3,))
+    vs = _rows("v", v, dtype, dev, shape)
+    T, H, d = shape
+    kc = _plain("k_cache", k_cache, dtype, dev, (None, H, None, d))
+    cache = k_cache.shape
+    vc = _plain("v_cache", v_cache, dtype, dev, cache)
+    sl = _plain("slots", slots, torch.int64, dev, (T,))
+    tab, n_pos, rot, p = _rotation(table, pos, T, dev)
+    wk = None if k_weight is None else _plain("k_weight", k_weight, dtype, dev, (d,))
+    _call("slh_kv_append", dev, stream,
+          (k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], _DTYPES[dtype], T, H, d, wk, eps, tab, n_pos, rot,
+           p, interleaved, kc, vc, cache[0], cache[2], sl))
     return k_cache, v_cache
 
 
-def _workspace(workspace, need, device):
-    """(tensor, pointer) of a workspace of `need` bytes: the given one, or a new one."""
-    if need < 0:
-        raise SLHError("sizes that the library does not take")
-    if need == 0:
+def _workspace(need, dev, workspace, device, stream):
+    """(tensor, address) of `need` bytes: of the workspace given, or of a new one."""
+    if need <= 0:
         return None, None
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    else:
-        _plain("workspace", workspace, torch.uint8, device, (None,))
-        if workspace.numel() < need:
-            raise SLHError(f"workspace must hold {need} bytes")
-    return workspace, workspace.data_ptr()
+        workspace = _empty(need, torch.uint8, device, stream)
+        return workspace, workspace.data_ptr()
+    at = _plain("workspace", workspace, torch.uint8, dev, (None,))
+    if workspace.numel() < need:
+        raise SLHError(f"workspace must hold {need} bytes")
+    return workspace, at
+
+
+def _bytes(name, dev, args):
+    """What a workspace function says for device `dev`."""
+    f = getattr(B.load(), name)
+    if torch.cuda.current_device() == dev:
+        return f(*args)
+    with torch.cuda.device(dev):
+        return f(*args)
 
 
 def slh_attend_workspace(Tq, Tk, B_, Hq, Hkv, d):
@@ -170,45 +182,31 @@ def slh_attend(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None, lse_
     at rows cu_q[b]..cu_q[b + 1] of q and cu_k[b]..cu_k[b + 1] of k and v (int32; cu_k None: as cu_q).
     causal: a sequence's last query sees all its keys, the one before it one fewer, and so on.
     scale: 1 / sqrt(d) by default.  lse_out: [Tq, Hq] float32.  Returns out."""
-    _rows("q", q)
-    _rows("k", k, 3, q)
-    _rows("v", v, 3, q, k.shape)
-    if q.dtype not in _HALVES:
+    dtype, dev, shape, qs = _first("q", q, (3,))
+    if dtype not in _HALVES:
         raise SLHError("q must be bfloat16 or float16")
-    Tq, Hq, d = q.shape
-    Tk, Hkv, dk = k.shape
-    if dk != d:
-        raise SLHError("q and k must have the same head size")
-    if cu_k is None:
-        cu_k = cu_q
-    dev = q.device
-    _plain("cu_q", cu_q, torch.int32, dev, (None,))
-    _plain("cu_k", cu_k, torch.int32, dev, cu_q.shape)
+    Tq, Hq, d = shape
+    if not isinstance(k, torch.Tensor) or k.dim() != 3 or k.shape[2] != d:
+        raise SLHError("k must have three dimensions and q's head size")
+    kshape = k.shape
+    ks = _rows("k", k, dtype, dev, kshape)
+    vs = _rows("v", v, dtype, dev, kshape)
+    Tk, Hkv, _ = kshape
+    cq = _plain("cu_q", cu_q, torch.int32, dev, (None,))
     n = cu_q.shape[0] - 1
+    ck = cq if cu_k is None else _plain("cu_k", cu_k, torch.int32, dev, (n + 1,))
     if n < 0:
         raise SLHError("cu_q must have an entry more than there are sequences")
     if out is None:
-        out = torch.empty((Tq, Hq, d), dtype=q.dtype, device=dev)
-    else:
-        _rows("out", out, 3, q, q.shape)
-    if lse_out is not None:
-        _plain("lse_out", lse_out, torch.float32, dev, (Tq, Hq))
-    lib = B.load()
-    with torch.cuda.device(dev):
-        need = lib.slh_attend_workspace(Tq, Tk, n, Hq, Hkv, d)
-        st = _stream(stream, dev)
-        if stream is not None and workspace is None:
-            with torch.cuda.stream(stream):
-                workspace, ws = _workspace(None, need, dev)
-        else:
-            workspace, ws = _workspace(workspace, need, dev)
-        rc = lib.slh_attend(q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(), k.stride(0), k.stride(1),
-                            v.data_ptr(), v.stride(0), v.stride(1), _DTYPES[q.dtype], Tq, Tk, n, Hq, Hkv, d,
-                            cu_q.data_ptr(), cu_k.data_ptr(), 1.0 / math.sqrt(d) if scale is None else scale,
-                            int(causal), out.data_ptr(), out.stride(0), out.stride(1), _address(lse_out), ws, need,
-                            st)
-    if rc != B.SLH_OK:
-        _fail("slh_attend", rc)
+        out = _empty(shape, dtype, q.device, stream)
+    os = _rows("out", out, dtype, dev, shape)
+    lse = None if lse_out is None else _plain("lse_out", lse_out, torch.float32, dev, (Tq, Hq))
+    need = _bytes("slh_attend_workspace", dev, (Tq, Tk, n, Hq, Hkv, d))
+    workspace, ws = _workspace(need, dev, workspace, q.device, stream)
+    _call("slh_attend", dev, stream,
+          (q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], _DTYPES[dtype], Tq, Tk,
+           n, Hq, Hkv, d, cq, ck, 1.0 / math.sqrt(d) if scale is None else scale, causal, out.data_ptr(), os[0],
+           os[1], lse, ws, need))
     return out
 
 
@@ -223,53 +221,40 @@ def slh_attend_paged(q, k_cache, v_cache, page_table, lens, prefix_pages=None, p
     [pages, Hkv, page, d]: sequence b's keys are the first prefix_len rows of prefix_pages (int32,
     shared by all), then the first lens[b] rows of its own pages page_table[b] (int32 [B, n]), the new
     tokens' rows the last of them.  lse_out: q's shape without d, float32.  Returns out."""
-    _rows("q", q, q.dim() if isinstance(q, torch.Tensor) and q.dim() in (3, 4) else 4)
-    if q.dtype not in _HALVES:
+    dtype, dev, shape, qs = _first("q", q, (3, 4))
+    if dtype not in _HALVES:
         raise SLHError("q must be bfloat16 or float16")
-    dev = q.device
+    n, Hq, d = shape[0], shape[-2], shape[-1]
+    n_q = shape[1] if len(shape) == 4 else 1
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    else:
-        _rows("out", out, q.dim(), q, q.shape)
-    n, Hq, d = q.shape[0], q.shape[-2], q.shape[-1]
-    n_q = q.shape[1] if q.dim() == 4 else 1
-    if n_q > 1 and n > 1:
-        for name, t in (("q", q), ("out", out)):
-            if t.stride(0) != n_q * t.stride(1):
-                raise SLHError(f"{name}: sequences must follow one another as their tokens do")
+        out = _empty(shape, dtype, q.device, stream)
+    os = _rows("out", out, dtype, dev, shape)
+    if n_q > 1 and n > 1 and (qs[0] != n_q * qs[1] or os[0] != n_q * os[1]):
+        raise SLHError("q and out: sequences must follow one another as their tokens do")
     at = 1 if n_q > 1 else 0                # the dimension whose stride is a token's
-    _plain("k_cache", k_cache, q.dtype, dev, (None, None, None, d))
-    _plain("v_cache", v_cache, q.dtype, dev, k_cache.shape)
-    pages, Hkv, page, _ = k_cache.shape
-    if not isinstance(page_table, torch.Tensor) or page_table.dtype != torch.int32 or page_table.device != dev \
-            or page_table.dim() != 2 or page_table.shape[0] != n or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-        raise SLHError(f"page_table must be an int32 tensor ({n}, *) on {dev} with unit stride in the last dimension")
+    kc = _plain("k_cache", k_cache, dtype, dev, (None, None, None, d))
+    cache = k_cache.shape
+    vc = _plain("v_cache", v_cache, dtype, dev, cache)
+    pages, Hkv, page, _ = cache
+    if not isinstance(page_table, torch.Tensor) or page_table.dtype is not torch.int32 \
+            or page_table.get_device() != dev or page_table.dim() != 2 or page_table.shape[0] != n \
+            or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise SLHError(f"page_table must be an int32 tensor ({n}, *) on device {dev} with unit stride in the last dimension")
     most = page_table.shape[1]
     ld = page_table.stride(0) if n > 1 else max(most, 1)
-    _plain("lens", lens, torch.int32, dev, (n,))
-    prefix_len = int(prefix_len)
+    ln = _plain("lens", lens, torch.int32, dev, (n,))
+    pre = None
     if prefix_len:
         if prefix_pages is None:
             raise SLHError("prefix_pages must be given with a prefix_len")
-        _plain("prefix_pages", prefix_pages, torch.int32, dev, (None,))
+        pre = _plain("prefix_pages", prefix_pages, torch.int32, dev, (None,))
         if prefix_len < 0 or prefix_pages.shape[0] * page < prefix_len:
             raise SLHError("prefix_pages hold fewer rows than prefix_len")
-    if lse_out is not None:
-        _plain("lse_out", lse_out, torch.float32, dev, q.shape[:-1])
-    lib = B.load()
-    with torch.cuda.device(dev):
-        need = lib.slh_attend_paged_workspace(n, n_q, Hq, Hkv, d, most * page, prefix_len)
-        st = _stream(stream, dev)
-        if stream is not None and workspace is None:
-            with torch.cuda.stream(stream):
-                workspace, ws = _workspace(None, need, dev)
-        else:
-            workspace, ws = _workspace(workspace, need, dev)
-        rc = lib.slh_attend_paged(q.data_ptr(), q.stride(at), q.stride(-2), k_cache.data_ptr(), v_cache.data_ptr(),
-                                  _DTYPES[q.dtype], pages, page, n, n_q, Hq, Hkv, d, page_table.data_ptr(), ld, most,
-                                  lens.data_ptr(), _address(prefix_pages) if prefix_len else None, prefix_len,
-                                  1.0 / math.sqrt(d) if scale is None else scale, out.data_ptr(), out.stride(at),
-                                  out.stride(-2), _address(lse_out), ws, need, st)
-    if rc != B.SLH_OK:
-        _fail("slh_attend_paged", rc)
+    lse = None if lse_out is None else _plain("lse_out", lse_out, torch.float32, dev, shape[:-1])
+    need = _bytes("slh_attend_paged_workspace", dev, (n, n_q, Hq, Hkv, d, most * page, prefix_len))
+    workspace, ws = _workspace(need, dev, workspace, q.device, stream)
+    _call("slh_attend_paged", dev, stream,
+          (q.data_ptr(), qs[at], qs[-2], kc, vc, _DTYPES[dtype], pages, page, n, n_q, Hq, Hkv, d,
+           page_table.data_ptr(), ld, most, ln, pre, prefix_len, 1.0 / math.sqrt(d) if scale is None else scale,
+           out.data_ptr(), os[at], os[-2], lse, ws, need))
     return out

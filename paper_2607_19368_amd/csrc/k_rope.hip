@@ -217,7 +217,7 @@ static bool rope_common_ok(int dtype, int64_t T, int64_t heads, int d, const voi
   if (((uintptr_t)w0) % 16 != 0 || ((uintptr_t)w1) % 16 != 0) return false;
   if (!(eps >= 0.0) || std::isinf(eps)) return false;
   if (!table) return rot == 0;
-  return ((uintptr_t)table) % 16 == 0 && pos && n_pos >= 1 && rot >= 16 && rot <= d && rot % 16 == 0;
+  return ((uintptr_t)table) % 16 == 0 && (pos || T == 0) && n_pos >= 1 && rot >= 16 && rot <= d && rot % 16 == 0;
 }
 
 struct RopeFreqs { double f[128]; };

@@ -116,6 +116,13 @@ def test_norm_of_zero_rows_and_of_no_tokens():
     y, _ = P.slh_qk_norm_rope(x, q_weight=w)
     assert not bool(y.any())
     assert P.slh_qk_norm_rope(x[:0], q_weight=w)[0].shape == (0, 2, 128)
+    table, none = P.slh_rope_table(4, 64), torch.empty(0, dtype=torch.int32).cuda()
+    assert P.slh_qk_norm_rope(x[:0], x[:0], w, w, table=table, pos=none)[1].shape == (0, 2, 128)
+    kc = torch.zeros(1, 2, 16, 128, dtype=BF).cuda()
+    P.slh_kv_append(x[:0], x[:0], kc, kc.clone(), none.long(), table=table, pos=none)
+    cu = torch.tensor([0], dtype=torch.int32).cuda()
+    assert P.slh_attend(x[:0], x[:0], x[:0], cu).shape == (0, 2, 128)
+    assert P.slh_attend_paged(x[:0], kc, kc, none.view(0, 1), none).shape == (0, 2, 128)
 
 
 # ---------------------------------------------------------------- cache append
