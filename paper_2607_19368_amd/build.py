@@ -34,6 +34,8 @@ SOURCES = [
     "slh_noalloc.hip",
     "k_rope.hip",
     "k_attend.hip",
+    "k_attend_rows.hip",
+    "attend_api.cpp",
 ]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

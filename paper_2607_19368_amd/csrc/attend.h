@@ -1,0 +1,220 @@
+// What the attention kernels share: element types, arguments, and which rows and keys a block
+// works on.
+#pragma once
+#include "slh_device.h"
+#include "slh_internal.h"
+
+#include "slh.h"
+
+namespace slh {
+
+typedef __bf16 at_bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 at_f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 at_f16x4 __attribute__((ext_vector_type(4)));
+typedef float at_f32x16 __attribute__((ext_vector_type(16)));
+typedef float at_f32x4 __attribute__((ext_vector_type(4)));
+typedef short at_s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t at_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t at_u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) at_s16x4* at_tr_ptr;
+typedef __attribute__((address_space(4))) const int* at_const_ints;
+typedef __attribute__((address_space(1))) const void* at_gptr;
+typedef __attribute__((address_space(3))) void* at_lptr;
+
+struct AtBf16 {
+  typedef at_bf16x8 vec;
+  static constexpr uint32_t EXP = 0x7f807f80u;       // exponent bits of two elements
+  static constexpr uint32_t CARRY = 0x00800080u;     // carries into the sign bit from a full exponent
+  __device__ static at_f32x16 mfma(at_u32x4 a, at_u32x4 b, at_f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(vec, a), __builtin_bit_cast(vec, b), c, 0, 0, 0);
+  }
+  __device__ static at_f32x4 mfma16(at_u32x4 a, at_u32x4 b, at_f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(vec, a), __builtin_bit_cast(vec, b), c, 0, 0, 0);
+  }
+  __device__ static at_f32x4 mfma16k16(at_u32x2 a, at_u32x2 b, at_f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(at_s16x4, a), __builtin_bit_cast(at_s16x4, b), c, 0, 0, 0);
+  }
+  __device__ static uint32_t pack(float lo, float hi) {
+    typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, (v2{(__bf16)lo, (__bf16)hi}));
+  }
+  __device__ static float value(uint16_t b) { return bf16_to_f32(b); }
+};
+struct AtF16 {
+  typedef at_f16x8 vec;
+  static constexpr uint32_t EXP = 0x7c007c00u;
+  static constexpr uint32_t CARRY = 0x04000400u;
+  __device__ static at_f32x16 mfma(at_u32x4 a, at_u32x4 b, at_f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(vec, a), __builtin_bit_cast(vec, b), c, 0, 0, 0);
+  }
+  __device__ static at_f32x4 mfma16(at_u32x4 a, at_u32x4 b, at_f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(vec, a), __builtin_bit_cast(vec, b), c, 0, 0, 0);
+  }
+  __device__ static at_f32x4 mfma16k16(at_u32x2 a, at_u32x2 b, at_f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(at_f16x4, a), __builtin_bit_cast(at_f16x4, b), c, 0, 0, 0);
+  }
+  __device__ static uint32_t pack(float lo, float hi) {
+    typedef _Float16 v2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, (v2{(_Float16)lo, (_Float16)hi}));
+  }
+  __device__ static float value(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
+};
+
+struct AttendArgs {
+  const uint16_t* q;      // element (token, head, e) at token q_st + head q_sh + e
+  int64_t q_st, q_sh;
+  const uint16_t* k;      // packed: element (token, head, e) by strides; paged: the cache
+  const uint16_t* v;      //   [n_pages][Hkv][page][d]
+  int64_t k_st, k_sh, v_st, v_sh;
+  uint16_t* out;          // as q
+  int64_t o_st, o_sh;
+  float* lse;             // [tokens][Hq] or NULL
+  int Hq, Hkv, g;         // g = Hq / Hkv
+  float c;                // scale log2(e)
+  float scale;
+  int B, causal;
+  // packed
+  const int* cu_q;        // [B + 1]
+  const int* cu_k;
+  int64_t Tq, Tk;
+  // paged
+  const int* pages;       // [B][ld_pages]
+  int64_t ld_pages;
+  int max_pages;
+  const int* lens;        // [B]
+  const int* prefix_pages;
+  int n_q, prefix_len, n_pages, lg_page;
+  // keys split over blocks: partial results of each split, joined by k_attend_join
+  int splits;             // of a packed sequence's or of a paged sequence's own keys
+  int pre_splits;         // of the prefix, slots in front of the others
+  int pre_tiles;          // row tiles of the prefix in this launch (0: not in it)
+  int64_t rows;           // tokens * Hq
+  float* part_o;          // [slot][rows][d] sum p v, NULL: one split, results go to out
+  float* part_ml;         // [slot][rows][2] maximum (of the unscaled scores) and sum p
+};
+
+// Transposing LDS read of 16 lanes: 4 rows of 16 elements, lane i gets column i.  `restrict` says
+// (as it is inlined) that no load in flight to LDS writes what is read here; without it the
+// compiler waits for all of them, the next tile's included.
+__device__ __forceinline__ at_u32x2 at_tr_read(const uint16_t* __restrict__ p) {
+  return __builtin_bit_cast(at_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_tr_ptr)p));
+}
+
+// A row's weights are taken relative to a maximum that may lag behind by up to 2^AT_LAG: the
+// accumulated sums are rescaled only when some row of the wave passes it.  Weights up to 2^8
+// lose nothing: their rounding is relative, and fp16 holds up to 2^15.
+constexpr float AT_LAG = 8.f;
+
+// A tile's rows are reached by 32-bit offsets in bytes from its first.
+constexpr int64_t AT_STRIDE = (int64_t)1 << 24;
+
+// What one block works on: rows [r0, r1) of the n_tok * g of a run of tokens, against nk keys.
+struct AtTask {
+  int64_t tok0;           // first token in q and out
+  int64_t key0;           // packed: first key's token
+  int r0, r1;
+  int nk;                 // keys that exist
+  int base, floor;        // token i sees the keys below max(floor, base + i + 1)
+  const int* list;        // paged: the pages
+  int split, n_split, slot;
+};
+
+// The sequence and row tile of a packed batch's block `at`: sequence b has
+// ceil(len_b g / ROWS) tiles, counted by 64 lanes at a time.  False: no such tile.
+template <int ROWS>
+__device__ __forceinline__ bool at_find(const AttendArgs& a, int at, AtTask& t) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int b = b0 + lane;
+    int lo = 0, n = 0;
+    if (b < a.B) {
+      lo = min((int64_t)max(a.cu_q[b], 0), a.Tq);
+      n = max(0, (int)min((int64_t)a.cu_q[b + 1], a.Tq) - lo);
+    }
+    const int tiles = (int)(((int64_t)n * a.g + ROWS - 1) / ROWS);
+    int upto = tiles;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int o = __shfl_up(upto, s);
+      if (lane >= s) upto += o;
+    }
+    const unsigned long long hit = __ballot(upto > at);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int nb = __builtin_amdgcn_readlane(n, l);
+      // the last rows of a causal sequence see the most keys: they go first
+      const int tile = __builtin_amdgcn_readlane(upto, l) - 1 - at;
+      t.tok0 = __builtin_amdgcn_readlane(lo, l);
+      const int kb = b0 + l;
+      const int64_t k0 = min((int64_t)max(a.cu_k[kb], 0), a.Tk);
+      t.key0 = k0;
+      t.nk = max(0, (int)(min((int64_t)a.cu_k[kb + 1], a.Tk) - k0));
+      t.r0 = tile * ROWS;
+      t.r1 = min(nb * a.g, t.r0 + ROWS);
+      t.base = a.causal ? t.nk - nb : t.nk - 1;
+      t.floor = a.causal ? 0 : t.nk;
+      return true;
+    }
+    at -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// The task of a block.  Blocks are dealt to the XCDs in turn: the key/value head varies fastest,
+// so that the blocks which read one head's keys meet in few of the XCDs' L2 caches.
+template <bool PAGED, int ROWS>
+__device__ __forceinline__ bool at_task(const AttendArgs& a, AtTask& t, int& kvh) {
+  int x = blockIdx.x;
+  kvh = x % a.Hkv;
+  x /= a.Hkv;
+  if (PAGED) {
+    if (x < a.pre_tiles * a.pre_splits) {    // every sequence's tokens against the prefix
+      t.split = x % a.pre_splits;
+      x /= a.pre_splits;
+      t.n_split = a.pre_splits;
+      t.slot = t.split;
+      t.tok0 = 0;
+      t.r0 = x * ROWS;
+      t.r1 = min(a.B * a.n_q * a.g, t.r0 + ROWS);
+      t.nk = t.floor = a.prefix_len;
+      t.base = 0;
+      t.list = a.prefix_pages;
+    } else {                                 // one sequence's tokens against its own keys
+      x -= a.pre_tiles * a.pre_splits;
+      t.split = x % a.splits;
+      x /= a.splits;
+      t.n_split = a.splits;
+      t.slot = a.pre_splits + t.split;
+      const int tiles = (a.n_q * a.g + ROWS - 1) / ROWS;
+      const int b = x / tiles;
+      t.tok0 = (int64_t)b * a.n_q;
+      t.r0 = (x - b * tiles) * ROWS;
+      t.r1 = min(a.n_q * a.g, t.r0 + ROWS);
+      t.nk = min(max(a.lens[b], 0), a.max_pages << a.lg_page);
+      t.base = t.nk - a.n_q;
+      t.floor = 0;
+      t.list = a.pages + b * a.ld_pages;
+    }
+    t.key0 = 0;
+    return true;
+  }
+  t.split = x % a.splits;
+  t.n_split = a.splits;
+  t.slot = t.split;
+  return at_find<ROWS>(a, x / a.splits, t);
+}
+
+// limits of a task's tokens: token i sees the first at_sees() keys
+__device__ __forceinline__ int at_sees(const AtTask& t, int i) {
+  return min(t.nk, max(t.floor, t.base + i + 1));
+}
+
+// ---- k_attend.hip: tiles of many rows; k_attend_rows.hip: few rows, keys over the waves ----
+constexpr int AT_WAVES = 4;                // waves of a block, of both
+constexpr int AT_ROWS = 32 * AT_WAVES;     // rows of a block of the first
+// d, paged, bf16 and rows (16 or 32) pick the instantiation; `blocks` as the tasks need
+hipError_t launch_attend_tiles(const AttendArgs& a, bool paged, bool bf16, int d, int64_t blocks, hipStream_t s);
+hipError_t launch_attend_rows(const AttendArgs& a, bool paged, bool bf16, int rows, int d, int64_t blocks, hipStream_t s);
+hipError_t launch_attend_join(const AttendArgs& a, bool bf16, int d, int slots, hipStream_t s);
+
+}  // namespace slh

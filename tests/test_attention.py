@@ -259,6 +259,20 @@ def test_attend_lowest_and_equal_scores():
 
 
 @gpu
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+def test_attend_again_gives_the_same_bits(dt, d):
+    """Few rows and many, masked and whole steps: a result read before its product is done, or a
+    buffer refilled while it is read, would differ from run to run."""
+    g = _gen(d)
+    for lq, lk, Hq, Hkv in (([65, 33, 7], [65, 200, 90], 4, 2), ([1300, 900], [1300, 2100], 28, 4)):
+        cq, ck = (torch.tensor([0] + x, dtype=torch.int32).cumsum(0).int().cuda() for x in (lq, lk))
+        q, k, v = (torch.randn(n, h, d, generator=g).to(dt).cuda() for n, h in ((sum(lq), Hq), (sum(lk), Hkv), (sum(lk), Hkv)))
+        want = P.slh_attend(q, k, v, cq, ck)
+        assert all(torch.equal(P.slh_attend(q, k, v, cq, ck), want) for _ in range(4))
+
+
+@gpu
 def test_attend_on_another_stream_and_in_a_graph():
     g = _gen(8)
     n = 200
