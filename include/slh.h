@@ -537,7 +537,8 @@ int slh_kv_append(const void *k, int64_t k_st, int64_t k_sh, const void *v, int6
  * preparation), which no other call may use until this one has run; the size is for the current
  * device.  Rows of out that belong to no sequence are not written.
  */
-int64_t slh_attend_workspace(int64_t Tq, int64_t Tk, int32_t B, int32_t Hq, int32_t Hkv, int32_t d);
+int64_t slh_attend_workspace(int64_t Tq, int64_t Tk, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                             int32_t causal);
 int slh_attend(const void *q, int64_t q_st, int64_t q_sh, const void *k, int64_t k_st, int64_t k_sh,
                const void *v, int64_t v_st, int64_t v_sh, int32_t dtype, int64_t Tq, int64_t Tk,
                int32_t B, int32_t Hq, int32_t Hkv, int32_t d, const int32_t *cu_q,

@@ -171,9 +171,9 @@ def _bytes(name, dev, args):
         return f(*args)
 
 
-def slh_attend_workspace(Tq, Tk, B_, Hq, Hkv, d):
+def slh_attend_workspace(Tq, Tk, B_, Hq, Hkv, d, causal=True):
     """Bytes that slh_attend needs as workspace on the current device."""
-    return int(B.load().slh_attend_workspace(Tq, Tk, B_, Hq, Hkv, d))
+    return int(B.load().slh_attend_workspace(Tq, Tk, B_, Hq, Hkv, d, causal))
 
 
 def slh_attend(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None, lse_out=None, workspace=None,
@@ -201,7 +201,7 @@ def slh_attend(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None, lse_
         out = _empty(shape, dtype, q.device, stream)
     os = _rows("out", out, dtype, dev, shape)
     lse = None if lse_out is None else _plain("lse_out", lse_out, torch.float32, dev, (Tq, Hq))
-    need = _bytes("slh_attend_workspace", dev, (Tq, Tk, n, Hq, Hkv, d))
+    need = _bytes("slh_attend_workspace", dev, (Tq, Tk, n, Hq, Hkv, d, causal))
     workspace, ws = _workspace(need, dev, workspace, q.device, stream)
     _call("slh_attend", dev, stream,
           (q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], _DTYPES[dtype], Tq, Tk,

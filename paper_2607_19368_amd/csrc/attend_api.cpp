@@ -26,6 +26,7 @@ struct AttendPart {
   int rows;               // of a block: AT_ROWS (k_attend), 32 or 16 (k_attend_rows)
   int splits;
   int64_t tiles;          // row tiles of a key/value head, all sequences together
+  double us;
 };
 struct AttendPlan {
   AttendPart own, pre;    // of the packed or the sequences' own keys; of the prefix (tiles 0: none)
@@ -33,11 +34,49 @@ struct AttendPlan {
   int64_t bytes;
 };
 
-// Key splits for `blocks` blocks over `keys` keys: two blocks a compute unit, each with `least` keys
-// or more.
-static int attend_splits(int64_t blocks, int64_t keys, int least, int n_cu) {
-  const int64_t fill = 2 * (int64_t)n_cu / std::max<int64_t>(1, blocks);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(fill, keys / least), 64));
+// What a launch costs, in microseconds, as measured with d = 128 on 256 compute units.  A block goes
+// through its keys 64 at a time: a tile of k_attend, or a step of each wave of k_attend_rows.  `start`:
+// of the launch, of finding rows and keys, of the first loads and the last stores; `one`: a block's 64
+// keys where it has a compute unit nearly to itself; `full`: a unit's 64 keys of one block, two
+// resident.  Measured against it, graph replays, us (model in brackets):
+//   queries x context, heads     16 rows        32 rows       128 rows
+//   512 x 0, 28 / 4              16.3 (16)      13.0 (13)     17 (17)
+//   1024 x 0, 28 / 4             37.2 (37)      28.7 (29)     27 (27)
+//   16 x 16384, 28 / 4           30.0           34.6 (31)     22.5 (24)
+//   1 x 32768, 28 / 4            22.9           24.7          25.7
+struct AttendCost { int rows; double start, one, full; };
+static const AttendCost ATTEND_COSTS[3] = {{16, 6.5, 0.65, 0.52}, {32, 7.0, 0.75, 0.72}, {AT_ROWS, 6.5, 1.3, 1.05}};
+// Partial results: two more passes over memory, and a launch.
+static double attend_join_us(int64_t slots, int64_t rows, int d) {
+  return slots > 1 ? 4.0 + 2.0 * (double)(slots * rows) * (4.0 * d + 8.0) / 3.5e6 : 0.0;
+}
+
+// The kernel and the splits that cost least for `sets` runs of `rows` rows a key/value head against `keys` keys
+// each, of which a row tile sees `mean` on average.  out_rows: rows of a partial result.  also: other
+// partial results of a row; same: the kernel of a launch that this one would join.
+static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys, double mean, int64_t out_rows, int d, int n_cu,
+                              int also, int same) {
+  AttendPart best = {};
+  best.us = INFINITY;
+  best.rows = 16, best.splits = 1;
+  const double work = d / 128.0, part = keys > 0 ? mean / (double)keys : 1.0;
+  const int64_t units = (keys + 63) / 64, most = std::max<int64_t>(1, std::min<int64_t>(64, units)), slots = 2 * (int64_t)n_cu;
+  for (const AttendCost& c : ATTEND_COSTS) {
+    const int64_t per = std::max<int64_t>(1, (rows + c.rows - 1) / c.rows), tiles = sets * per, base = tiles * Hkv;
+    // a unit's 64 keys come from memory at 5.2 TB/s, once for the row tiles that share them
+    const double full = std::max(c.full * work, 256.0 * d * n_cu / 5.2e6 / (double)per), one = std::max(c.one * work, full);
+    const int64_t fill = slots / std::max<int64_t>(1, base);
+    for (const int64_t want : {(int64_t)1, (int64_t)2, (int64_t)3, fill / 2, fill, 2 * fill, 4 * fill, most}) {
+      const int64_t s = std::max<int64_t>(1, std::min(want, most)), n = (units + s - 1) / s, blocks = base * s;
+      const int64_t rounds = blocks / slots, rest = blocks - rounds * slots;
+      const double each = (double)n * part;
+      double us = (double)rounds * each * 2.0 * full + (rest == 0 ? 0.0 : each * (rest <= n_cu ? one : 2.0 * full));
+      if (part < 1.0 && rounds > 1) us = (double)blocks * each * full / n_cu + each * full;    // uneven blocks fill in
+      us = std::max(us, (double)n * c.one * work) + (c.rows == same ? 0.0 : c.start) + attend_join_us(s + also, out_rows, d);
+      if (us < best.us) best = AttendPart{c.rows, (int)s, tiles, us};
+    }
+  }
+  return best;
 }
 
 static void attend_finish(AttendPlan& p, int64_t rows, int d) {
@@ -45,34 +84,25 @@ static void attend_finish(AttendPlan& p, int64_t rows, int d) {
   p.bytes = p.slots > 1 ? p.slots * rows * (4 * (int64_t)d + 8) : 0;
 }
 
-static AttendPlan attend_plan_packed(int64_t Tq, int64_t Tk, int B, int Hq, int Hkv, int d) {
-  const int n_cu = attend_cus();
-  const int64_t rows = Tq * (Hq / Hkv), keys = Tk / std::max(1, B);
+static AttendPlan attend_plan_packed(int64_t Tq, int64_t Tk, int B, int Hq, int Hkv, int d, bool causal) {
   AttendPlan p = {};
-  p.own.rows = AT_ROWS;
-  // the tiles that there are at least; the keys of the average sequence
-  auto sure = [&](int r) { return std::max<int64_t>(B, (rows + r - 1) / r) * Hkv; };
-  if (sure(AT_ROWS) < n_cu && sure(32) * keys < (int64_t)4096 * n_cu) p.own.rows = rows * Hkv > 32 * n_cu ? 32 : 16;
-  const int r = p.own.rows;
-  p.own.tiles = rows / r + B;
-  p.own.splits = attend_splits(sure(r), keys, r == AT_ROWS ? 4 * 64 : 256, n_cu);
+  // as if the sequences were equal; where they are not, their tiles are B more at most
+  const int64_t rows = Tq * (Hq / Hkv), n = std::max(1, B), keys = Tk / n;
+  const double mean = causal ? std::max((double)keys / 2, (double)keys - (double)Tq / n / 2) : (double)keys;
+  p.own = attend_part((rows + n - 1) / n, n, Hkv, keys, mean, Tq * Hq, d, attend_cus(), 0, 0);
+  p.own.tiles = rows / p.own.rows + B;
   attend_finish(p, Tq * Hq, d);
   return p;
 }
 
 static AttendPlan attend_plan_paged(int B, int n_q, int Hq, int Hkv, int d, int64_t max_len, int64_t prefix_len) {
-  const int n_cu = attend_cus(), g = Hq / Hkv;
-  auto part = [&](int64_t rows, int64_t sets, int64_t keys) {
-    AttendPart p;
-    p.rows = rows <= 16 ? 16 : rows <= 64 ? 32 : AT_ROWS;
-    p.tiles = sets * ((rows + p.rows - 1) / p.rows);
-    p.splits = attend_splits(p.tiles * Hkv, keys, 256, n_cu);
-    return p;
-  };
   AttendPlan p = {};
-  p.own = part((int64_t)n_q * g, B, max_len);
-  if (prefix_len > 0) p.pre = part((int64_t)B * n_q * g, 1, prefix_len);
-  attend_finish(p, (int64_t)B * n_q * Hq, d);
+  const int n_cu = attend_cus();
+  const int64_t rows = (int64_t)n_q * (Hq / Hkv), out_rows = (int64_t)B * n_q * Hq;
+  p.own = attend_part(rows, B, Hkv, max_len, (double)max_len, out_rows, d, n_cu, prefix_len > 0, 0);
+  if (prefix_len > 0)
+    p.pre = attend_part(B * rows, 1, Hkv, prefix_len, (double)prefix_len, out_rows, d, n_cu, p.own.splits, p.own.rows);
+  attend_finish(p, out_rows, d);
   return p;
 }
 
@@ -129,10 +159,11 @@ static bool attend_common_ok(int dtype, int64_t B, int Hq, int Hkv, int d, doubl
 
 extern "C" {
 
-int64_t slh_attend_workspace(int64_t Tq, int64_t Tk, int32_t B, int32_t Hq, int32_t Hkv, int32_t d) {
+int64_t slh_attend_workspace(int64_t Tq, int64_t Tk, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                             int32_t causal) {
   using namespace slh;
   if (!attend_common_ok(SLH_BF16, B, Hq, Hkv, d, 1.0) || !attend_packed_ok(Tq, Tk, Hq / Hkv)) return SLH_EINVAL;
-  return attend_plan_packed(Tq, Tk, B, Hq, Hkv, d).bytes;
+  return attend_plan_packed(Tq, Tk, B, Hq, Hkv, d, causal != 0).bytes;
 }
 
 int slh_attend(const void* q, int64_t q_st, int64_t q_sh, const void* k, int64_t k_st, int64_t k_sh,
@@ -155,7 +186,7 @@ int slh_attend(const void* q, int64_t q_st, int64_t q_sh, const void* k, int64_t
   a.Hq = Hq, a.Hkv = Hkv, a.g = g, a.c = (float)(scale * 1.4426950408889634), a.scale = (float)scale, a.B = B, a.causal = causal != 0;
   a.cu_q = cu_q, a.cu_k = cu_k, a.Tq = Tq, a.Tk = Tk;
   a.rows = Tq * Hq;
-  return attend_run(a, attend_plan_packed(Tq, Tk, B, Hq, Hkv, d), false, dtype == SLH_BF16, d, workspace,
+  return attend_run(a, attend_plan_packed(Tq, Tk, B, Hq, Hkv, d, causal != 0), false, dtype == SLH_BF16, d, workspace,
                     workspace_bytes, (hipStream_t)stream);
 }
 

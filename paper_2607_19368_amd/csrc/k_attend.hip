@@ -177,6 +177,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend(AttendArgs a) {
       }
     };
     k_read(0);
+    __builtin_amdgcn_s_setprio(1);               // the wave whose turn the matrix unit is goes first
 #pragma unroll
     for (int st = 0; st < KS; ++st) {
       if (st + 1 < KS) k_read(st + 1);
@@ -184,6 +185,10 @@ __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend(AttendArgs a) {
       for (int kb = 0; kb < 2; ++kb) s[kb] = TY::mfma(kf[st & 1][kb], qf[st], s[kb]);
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
+    // The compiler spends the wait states between the last product and the first read of its scores.  Of
+    // ways of different length past a branch it may count only the first that it follows, unless
+    // that way alone is long enough: the 64 instructions of the one below are.
     if (masked) {
       int left = limit - j0 - 4 * half;
       asm volatile("" : "+v"(left));               // a branch, not 32 selects in every tile
@@ -245,6 +250,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend(AttendArgs a) {
       }
     };
     v_step(0);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kc = 0; kc < 4; ++kc) {
       if (kc < 3) v_step(kc + 1);
@@ -252,6 +258,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend(AttendArgs a) {
       for (int b = 0; b < DB; ++b) o[b] = TY::mfma(vf[kc & 1][b], pf[kc], o[b]);
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   // 0 x inf in the product would reach rows that do not see the key.  In a tile that some row of the
@@ -322,10 +329,10 @@ __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend(AttendArgs a) {
     const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(w[0]) + __uint_as_float(w[1]);
   }
-  if (!real) return;
   const bool empty = m == -INFINITY && l == 0.f;
   const int64_t r = (t.tok0 + i) * a.Hq + h;
   if (a.part_o) {
+    if (!real) return;
     const int64_t at = t.slot * a.rows + r;
     if (half == 0) {
       a.part_ml[2 * at] = m;
@@ -344,18 +351,20 @@ __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend(AttendArgs a) {
     return;
   }
   const float inv = empty ? 0.f : 1.0f / l;
-  uint16_t* op = a.out + (t.tok0 + i) * a.o_st + h * a.o_sh;
+  uint16_t* op = a.out + (t.tok0 + i) * a.o_st + h * a.o_sh + 8 * half;
 #pragma unroll
   for (int b = 0; b < DB; ++b)
 #pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      const int d = 32 * b + 8 * (e / 4) + 4 * half;
-      at_u32x2 w;
-      w[0] = TY::pack(o[b][e] * inv, o[b][e + 1] * inv);
-      w[1] = TY::pack(o[b][e + 2] * inv, o[b][e + 3] * inv);
-      if (d < D) *(at_u32x2*)(op + d) = w;
+    for (int e = 0; e < 16; e += 8) {
+      // the two halves hold elements 0..3 and 4..7 of two eights: they trade, and each stores one
+      const auto w0 = __builtin_amdgcn_permlane32_swap(TY::pack(o[b][e] * inv, o[b][e + 1] * inv),
+                                                       TY::pack(o[b][e + 4] * inv, o[b][e + 5] * inv), false, false);
+      const auto w1 = __builtin_amdgcn_permlane32_swap(TY::pack(o[b][e + 2] * inv, o[b][e + 3] * inv),
+                                                       TY::pack(o[b][e + 6] * inv, o[b][e + 7] * inv), false, false);
+      const int d = 32 * b + 2 * e;
+      if (real && d < D) *(at_u32x4*)(op + d) = at_u32x4{w0[0], w1[0], w0[1], w1[1]};
     }
-  if (a.lse && half == 0)
+  if (a.lse && real && half == 0)
     a.lse[r] = empty ? -INFINITY : m * a.scale + 0.69314718f * __builtin_amdgcn_logf(l);
 }
 

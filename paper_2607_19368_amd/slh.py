@@ -87,7 +87,7 @@ def load():
                              + [i32, i64, i32, vp, vp, f64, vp, i64, i32, vp, i32, vp]),
         "slh_kv_append": (i32, [vp, i64, i64, vp, i64, i64, i32, i64, i32, i32, vp, f64, vp, i64, i32, vp, i32,
                                 vp, vp, i64, i32, vp, vp]),
-        "slh_attend_workspace": (i64, [i64, i64, i32, i32, i32, i32]),
+        "slh_attend_workspace": (i64, [i64, i64, i32, i32, i32, i32, i32]),
         "slh_attend": (i32, [vp, i64, i64] * 3 + [i32, i64, i64, i32, i32, i32, i32, vp, vp, f64, i32, vp, i64, i64,
                                                   vp, vp, i64, vp]),
         "slh_attend_paged_workspace": (i64, [i32, i32, i32, i32, i32, i64, i64]),
