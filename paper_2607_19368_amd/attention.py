@@ -58,12 +58,11 @@ def _rows(name, t, dtype, dev, shape):
 
 
 def _plain(name, t, dtype, dev, shape):
-    """Address of t, a contiguous tensor of `shape` (an entry None: any length)."""
+    """Address of t, a contiguous tensor of `shape`, or of so many dimensions."""
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
         raise SLHError(f"{name} must be a contiguous {dtype} tensor on device {dev}")
-    have = t.shape
-    if have != shape and (len(have) != len(shape) or any(n is not None and n != m for n, m in zip(shape, have))):
-        raise SLHError(f"{name} must have shape ({', '.join('*' if n is None else str(n) for n in shape)})")
+    if t.shape != shape if shape.__class__ is not int else t.dim() != shape:
+        raise SLHError(f"{name} must have " + (f"{shape} dimensions" if isinstance(shape, int) else f"shape {tuple(shape)}"))
     return t.data_ptr()
 
 
@@ -79,10 +78,11 @@ def _rotation(table, pos, T, dev):
     """(table address, n_pos, rot_dim, pos address) of a rotation, or of none."""
     if table is None:
         return None, 0, 0, None
-    t = _plain("table", table, torch.float32, dev, (None, 2, None))
-    if pos is None:
-        raise SLHError("pos must be given with a table")
-    return t, table.shape[0], 2 * table.shape[2], _plain("pos", pos, torch.int32, dev, (T,))
+    t = _plain("table", table, torch.float32, dev, 3)
+    n_pos, two, half = table.shape
+    if two != 2 or pos is None:
+        raise SLHError("table must have shape (*, 2, rot_dim / 2), and pos must be given with it")
+    return t, n_pos, 2 * half, _plain("pos", pos, torch.int32, dev, (T,))
 
 
 def slh_rope_table(n_pos, rot_dim, base=10000.0, scaling=B.SLH_ROPE_PLAIN, factor=1.0, orig_len=0,
@@ -137,8 +137,10 @@ def slh_kv_append(k, v, k_cache, v_cache, slots, k_weight=None, eps=1e-6, table=
     dtype, dev, shape, ks = _first("k", k, (3,))
     vs = _rows("v", v, dtype, dev, shape)
     T, H, d = shape
-    kc = _plain("k_cache", k_cache, dtype, dev, (None, H, None, d))
+    kc = _plain("k_cache", k_cache, dtype, dev, 4)
     cache = k_cache.shape
+    if cache[1] != H or cache[3] != d:
+        raise SLHError(f"k_cache must have shape (*, {H}, *, {d})")
     vc = _plain("v_cache", v_cache, dtype, dev, cache)
     sl = _plain("slots", slots, torch.int64, dev, (T,))
     tab, n_pos, rot, p = _rotation(table, pos, T, dev)
@@ -156,7 +158,7 @@ def _workspace(need, dev, workspace, device, stream):
     if workspace is None:
         workspace = _empty(need, torch.uint8, device, stream)
         return workspace, workspace.data_ptr()
-    at = _plain("workspace", workspace, torch.uint8, dev, (None,))
+    at = _plain("workspace", workspace, torch.uint8, dev, 1)
     if workspace.numel() < need:
         raise SLHError(f"workspace must hold {need} bytes")
     return workspace, at
@@ -192,7 +194,7 @@ def slh_attend(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None, lse_
     ks = _rows("k", k, dtype, dev, kshape)
     vs = _rows("v", v, dtype, dev, kshape)
     Tk, Hkv, _ = kshape
-    cq = _plain("cu_q", cu_q, torch.int32, dev, (None,))
+    cq = _plain("cu_q", cu_q, torch.int32, dev, 1)
     n = cu_q.shape[0] - 1
     ck = cq if cu_k is None else _plain("cu_k", cu_k, torch.int32, dev, (n + 1,))
     if n < 0:
@@ -232,22 +234,29 @@ def slh_attend_paged(q, k_cache, v_cache, page_table, lens, prefix_pages=None, p
     if n_q > 1 and n > 1 and (qs[0] != n_q * qs[1] or os[0] != n_q * os[1]):
         raise SLHError("q and out: sequences must follow one another as their tokens do")
     at = 1 if n_q > 1 else 0                # the dimension whose stride is a token's
-    kc = _plain("k_cache", k_cache, dtype, dev, (None, None, None, d))
+    kc = _plain("k_cache", k_cache, dtype, dev, 4)
     cache = k_cache.shape
+    if cache[3] != d:
+        raise SLHError("k_cache must have q's head size")
     vc = _plain("v_cache", v_cache, dtype, dev, cache)
     pages, Hkv, page, _ = cache
     if not isinstance(page_table, torch.Tensor) or page_table.dtype is not torch.int32 \
-            or page_table.get_device() != dev or page_table.dim() != 2 or page_table.shape[0] != n \
-            or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-        raise SLHError(f"page_table must be an int32 tensor ({n}, *) on device {dev} with unit stride in the last dimension")
-    most = page_table.shape[1]
-    ld = page_table.stride(0) if n > 1 else max(most, 1)
+            or page_table.get_device() != dev or page_table.dim() != 2:
+        raise SLHError(f"page_table must be an int32 tensor of two dimensions on device {dev}")
+    rows, most = page_table.shape
+    ld, unit = page_table.stride()
+    if rows != n or (unit != 1 and most > 1):
+        raise SLHError(f"page_table must have shape ({n}, *) and unit stride in the last dimension")
+    if n < 2 or ld < most:
+        if n > 1:
+            raise SLHError("page_table: rows must not overlap")
+        ld = most
     ln = _plain("lens", lens, torch.int32, dev, (n,))
     pre = None
     if prefix_len:
         if prefix_pages is None:
             raise SLHError("prefix_pages must be given with a prefix_len")
-        pre = _plain("prefix_pages", prefix_pages, torch.int32, dev, (None,))
+        pre = _plain("prefix_pages", prefix_pages, torch.int32, dev, 1)
         if prefix_len < 0 or prefix_pages.shape[0] * page < prefix_len:
             raise SLHError("prefix_pages hold fewer rows than prefix_len")
     lse = None if lse_out is None else _plain("lse_out", lse_out, torch.float32, dev, shape[:-1])
