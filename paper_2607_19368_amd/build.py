@@ -35,6 +35,7 @@ SOURCES = [
     "k_rope.hip",
     "k_attend.hip",
     "k_attend_rows.hip",
+    "k_attend_both.hip",
     "attend_api.cpp",
 ]
 

@@ -164,8 +164,7 @@ __device__ __forceinline__ bool at_find(const AttendArgs& a, int at, AtTask& t) 
 // The task of a block.  Blocks are dealt to the XCDs in turn: the key/value head varies fastest,
 // so that the blocks which read one head's keys meet in few of the XCDs' L2 caches.
 template <bool PAGED, int ROWS>
-__device__ __forceinline__ bool at_task(const AttendArgs& a, AtTask& t, int& kvh) {
-  int x = blockIdx.x;
+__device__ __forceinline__ bool at_task(const AttendArgs& a, int x, AtTask& t, int& kvh) {
   kvh = x % a.Hkv;
   x /= a.Hkv;
   if (PAGED) {
@@ -213,9 +212,12 @@ __device__ __forceinline__ int at_sees(const AtTask& t, int i) {
 // ---- k_attend.hip: tiles of many rows; k_attend_rows.hip: few rows, keys over the waves ----
 constexpr int AT_WAVES = 4;                // waves of a block, of both
 constexpr int AT_ROWS = 32 * AT_WAVES;     // rows of a block of the first
-// d, paged, bf16 and rows (16 or 32) pick the instantiation; `blocks` as the tasks need
+// Both in one launch: the prefix in tiles, `pre_blocks` of them, the sequences' own keys by rows.
+// d, paged, bf16 and rows (16 or 32) pick the instantiation; `blocks` as the tasks need.
 hipError_t launch_attend_tiles(const AttendArgs& a, bool paged, bool bf16, int d, int64_t blocks, hipStream_t s);
 hipError_t launch_attend_rows(const AttendArgs& a, bool paged, bool bf16, int rows, int d, int64_t blocks, hipStream_t s);
+hipError_t launch_attend_both(const AttendArgs& a, bool bf16, int rows, int d, int64_t pre_blocks, int64_t blocks,
+                              hipStream_t s);
 hipError_t launch_attend_join(const AttendArgs& a, bool bf16, int d, int slots, hipStream_t s);
 
 }  // namespace slh

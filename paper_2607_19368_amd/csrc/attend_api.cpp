@@ -125,7 +125,9 @@ static int attend_run(AttendArgs& a, const AttendPlan& p, bool paged, bool bf16,
   (void)hipGetLastError();
   a.pre_tiles = (int)p.pre.tiles;
   hipError_t e;
-  if (pre && p.pre.rows != p.own.rows) {
+  if (pre && p.pre.rows == AT_ROWS && p.own.rows != AT_ROWS) {
+    e = launch_attend_both(a, bf16, p.own.rows, d, pre, pre + own, s);
+  } else if (pre && p.pre.rows != p.own.rows) {
     e = go(p.pre.rows, pre);
     if (e != hipSuccess) return SLH_EHIP;
     a.pre_tiles = 0;
