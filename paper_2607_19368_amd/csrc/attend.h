@@ -89,6 +89,7 @@ struct AttendArgs {
   int pre_splits;         // of the prefix, slots in front of the others
   int pre_tiles;          // row tiles of the prefix in this launch (0: not in it)
   int64_t rows;           // tokens * Hq
+  uint64_t by_heads, by_splits, by_pre_splits;   // at_divisor() of Hkv and the splits
   float* part_o;          // [slot][rows][d] sum p v, NULL: one split, results go to out
   float* part_ml;         // [slot][rows][2] maximum (of the unscaled scores) and sum p
 };
@@ -107,6 +108,11 @@ constexpr float AT_LAG = 8.f;
 
 // A tile's rows are reached by 32-bit offsets in bytes from its first.
 constexpr int64_t AT_STRIDE = (int64_t)1 << 24;
+
+// x / n for a block number x < 2^23 and n < 2^16: x ceil(2^40 / n) / 2^40, whose error x n / 2^40 is less than
+// the 1 / n by which it could reach the next whole number.
+inline uint64_t at_divisor(int n) { return (((uint64_t)1 << 40) + n - 1) / (uint64_t)n; }
+__device__ __forceinline__ int at_div(int x, uint64_t by) { return (int)(((uint64_t)(uint32_t)x * by) >> 40); }
 
 // What one block works on: rows [r0, r1) of the n_tok * g of a run of tokens, against nk keys.
 struct AtTask {
@@ -138,11 +144,14 @@ __device__ __forceinline__ bool at_find(const AttendArgs& a, int at, AtTask& t) 
       kn = max(0, (int)min((int64_t)k1, a.Tk) - klo);
     }
     int upto = (int)(((int64_t)n * a.g + ROWS - 1) / ROWS);
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-      const int o = __shfl_up(upto, s);
-      if (lane >= s) upto += o;
-    }
+    // inclusive sums over the lanes: shifts by 1, 2, 4 and 8 within rows of 16, then the last of
+    // each row, then of each half, added to the ones behind
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xF, 0xF, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xF, 0xF, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xF, 0xF, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xF, 0xF, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x142, 0xA, 0xF, false);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x143, 0xC, 0xF, false);
     const unsigned long long hit = __ballot(upto > at);
     if (hit) {
       const int l = __builtin_ctzll(hit);
@@ -165,12 +174,14 @@ __device__ __forceinline__ bool at_find(const AttendArgs& a, int at, AtTask& t) 
 // so that the blocks which read one head's keys meet in few of the XCDs' L2 caches.
 template <bool PAGED, int ROWS>
 __device__ __forceinline__ bool at_task(const AttendArgs& a, int x, AtTask& t, int& kvh) {
-  kvh = x % a.Hkv;
-  x /= a.Hkv;
+  const int all = x;
+  x = at_div(x, a.by_heads);
+  kvh = all - x * a.Hkv;
   if (PAGED) {
     if (x < a.pre_tiles * a.pre_splits) {    // every sequence's tokens against the prefix
-      t.split = x % a.pre_splits;
-      x /= a.pre_splits;
+      const int tile = at_div(x, a.by_pre_splits);
+      t.split = x - tile * a.pre_splits;
+      x = tile;
       t.n_split = a.pre_splits;
       t.slot = t.split;
       t.tok0 = 0;
@@ -181,12 +192,13 @@ __device__ __forceinline__ bool at_task(const AttendArgs& a, int x, AtTask& t, i
       t.list = a.prefix_pages;
     } else {                                 // one sequence's tokens against its own keys
       x -= a.pre_tiles * a.pre_splits;
-      t.split = x % a.splits;
-      x /= a.splits;
+      const int tile = at_div(x, a.by_splits);
+      t.split = x - tile * a.splits;
+      x = tile;
       t.n_split = a.splits;
       t.slot = a.pre_splits + t.split;
       const int tiles = (a.n_q * a.g + ROWS - 1) / ROWS;
-      const int b = x / tiles;
+      const int b = tiles == 1 ? x : x / tiles;
       t.tok0 = (int64_t)b * a.n_q;
       t.r0 = (x - b * tiles) * ROWS;
       t.r1 = min(a.n_q * a.g, t.r0 + ROWS);
@@ -198,10 +210,11 @@ __device__ __forceinline__ bool at_task(const AttendArgs& a, int x, AtTask& t, i
     t.key0 = 0;
     return true;
   }
-  t.split = x % a.splits;
+  const int tile = at_div(x, a.by_splits);
+  t.split = x - tile * a.splits;
   t.n_split = a.splits;
   t.slot = t.split;
-  return at_find<ROWS>(a, x / a.splits, t);
+  return at_find<ROWS>(a, tile, t);
 }
 
 // limits of a task's tokens: token i sees the first at_sees() keys

@@ -111,13 +111,16 @@ static int attend_run(AttendArgs& a, const AttendPlan& p, bool paged, bool bf16,
                       hipStream_t s) {
   if (p.bytes && (!ws || ((uintptr_t)ws) % 16 != 0 || ws_bytes < p.bytes)) return SLH_EINVAL;
   const int64_t own = p.own.tiles * p.own.splits * a.Hkv, pre = p.pre.tiles * p.pre.splits * a.Hkv;
-  if (own + pre > INT32_MAX / 256) return SLH_EINVAL;
+  if (own + pre > (1 << 23) - 64) return SLH_EINVAL;
   if (p.bytes) {
     a.part_o = (float*)ws;
     a.part_ml = a.part_o + p.slots * a.rows * d;
   }
   a.splits = p.own.splits;
   a.pre_splits = p.pre.tiles ? p.pre.splits : 0;
+  a.by_heads = at_divisor(a.Hkv);
+  a.by_splits = at_divisor(a.splits);
+  a.by_pre_splits = at_divisor(std::max(1, a.pre_splits));
   auto go = [&](int rows, int64_t blocks) {
     return rows == AT_ROWS ? launch_attend_tiles(a, paged, bf16, d, blocks, s)
                            : launch_attend_rows(a, paged, bf16, rows, d, blocks, s);
