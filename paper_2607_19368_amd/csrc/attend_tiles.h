@@ -209,9 +209,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
       if (next >= 0) load_tile(next, nbuf);
       scores(std::false_type{}, s, ck, nullptr, nullptr, nbuf);
     }
-    // The compiler spends the wait states between the last product and the first read of its scores.  Of
-    // ways of different length past a branch it may count only the first that it follows, unless
-    // that way alone is long enough: the 64 instructions of the one below are.
+    // (see at_products_done: of the ways past this branch the one through it is long enough by itself)
     if (masked) {
       int left = limit - j0 - 4 * half;
       asm volatile("" : "+v"(left));               // a branch, not 32 selects in every tile
@@ -346,6 +344,9 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     find_pages(min(tile + 2, t1 - 1));
   }
 
+  at_products_done(o[DB - 1]);
+#pragma unroll
+  for (int b = 0; b + 1 < DB; ++b) at_products_with(o[b]);
   {
     const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(w[0]) + __uint_as_float(w[1]);

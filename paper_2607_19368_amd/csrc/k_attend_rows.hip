@@ -42,6 +42,10 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
   const int lane = threadIdx.x & 63, half = lane >> 5, e = 4 * (lane & 31);
   const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= a.rows) return;
+  const int64_t tok = r / a.Hq;
+  const int h = (int)(r - tok * a.Hq);
+  // packed rows in front of the first sequence or behind the last have no results
+  if (a.cu_q && (tok < a.cu_q[0] || tok >= a.cu_q[a.B])) return;
   auto ml = [&](int s) { return *(const float2*)(a.part_ml + 2 * (s * a.rows + r)); };
   auto is_empty = [](float2 v) { return v.x == -INFINITY && v.y == 0.f; };
   const float2 none = make_float2(-INFINITY, 0.f);
@@ -90,8 +94,6 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
 #pragma unroll
   for (int c = 0; c < 4; ++c) o[c] += __shfl_xor(o[c], 32);
   const float inv = empty ? 0.f : 1.0f / l;
-  const int64_t tok = r / a.Hq;
-  const int h = (int)(r - tok * a.Hq);
   if (half == 0 && e < d)
     *(at_u32x2*)(a.out + tok * a.o_st + h * a.o_sh + e) =
         at_u32x2{TY::pack(o[0] * inv, o[1] * inv), TY::pack(o[2] * inv, o[3] * inv)};

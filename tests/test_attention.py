@@ -212,6 +212,27 @@ def test_attend_few_queries_many_keys(lq, lk):
 
 
 @gpu
+@pytest.mark.parametrize("lk", [30, 6000])          # in one piece, and with the keys split
+def test_attend_rows_of_no_sequence_and_wider_outputs(lk):
+    """Rows in front of the first sequence and behind the last are not written, nor what lies beside out."""
+    g = _gen(lk)
+    q = torch.randn(20, 4, 64, generator=g).to(BF)
+    k, v = (torch.randn(lk + 9, 2, 64, generator=g).to(BF) for _ in range(2))
+    wide, lse = torch.full((20, 5, 72), 7.0, dtype=BF).cuda(), torch.full((20, 4), 7.0).cuda()
+    cq, ck = torch.tensor([3, 5, 16], dtype=torch.int32), torch.tensor([4, 4 + lk // 3, 4 + lk], dtype=torch.int32)
+    P.slh_attend(q.cuda(), k.cuda(), v.cuda(), cq.cuda(), ck.cuda(), out=wide[:, 1:, :64], lse_out=lse)
+    for b in (0, 1):
+        rq, rk = slice(int(cq[b]), int(cq[b + 1])), slice(int(ck[b]), int(ck[b + 1]))
+        n, m = rq.stop - rq.start, rk.stop - rk.start
+        o, tol, e, etol = AP.attend(q[rq], k[rk], v[rk], [m - n + i + 1 for i in range(n)], 1 / 8)
+        _close(wide[rq, 1:, :64], o, tol)
+        assert bool(((lse[rq].double().cpu() - e).abs() <= etol).all())
+    wide[3:16, 1:, :64] = 7.0
+    lse[3:16] = 7.0
+    assert bool((wide == 7.0).all()) and bool((lse == 7.0).all())
+
+
+@gpu
 def test_attend_large_scores_and_scale():
     """Scores of several hundred: the running maximum moves by more than fp16 or exp can hold."""
     _attend_case([90], [90], 2, 1, 64, HF, True, 5, scale=8.0)
@@ -368,6 +389,29 @@ def test_paged_batches(B_, n_q, Hq, Hkv):
 def test_paged_long():
     _paged_case(2, 1, 8, 2, 128, BF, 64, 5000, [9000, 1], 4)
     _paged_case(1, 2, 4, 4, 128, HF, 32, 0, [20011], 5)
+
+
+@gpu
+@pytest.mark.parametrize("B_,prefix", [(3, 700), (40, 3000)])      # one launch of rows; tiles and rows
+def test_paged_strided_queries_and_outputs(B_, prefix):
+    g = _gen(B_)
+    page, Hkv, d, n_q = 16, 2, 96, 2
+    n = -(-prefix // page)
+    kc, vc = (torch.randn(n + B_ * 3, Hkv, page, d, generator=g).to(HF) for _ in range(2))
+    wide = torch.randn(B_ * n_q, 9, d, generator=g).to(HF)
+    out = torch.full((B_ * n_q, 9, d), 7.0, dtype=HF).cuda()
+    table = torch.empty(B_, 5, dtype=torch.int32)
+    table[:, :3] = n + torch.arange(B_ * 3).view(B_, 3)
+    lens = torch.randint(2, 49, (B_,), generator=g).int()
+    P.slh_attend_paged(wide.cuda().view(B_, n_q, 9, d)[:, :, 1:], kc.cuda(), vc.cuda(), table.cuda()[:, :3], lens.cuda(),
+                       torch.arange(n, dtype=torch.int32).cuda(), prefix, out=out.view(B_, n_q, 9, d)[:, :, 1:])
+    flat = [t.permute(0, 2, 1, 3).reshape(-1, Hkv, d) for t in (kc, vc)]
+    for b in range(0, B_, 7):
+        at = (n + 3 * b) * page
+        k, v = (torch.cat([t[:prefix], t[at:at + int(lens[b])]]) for t in flat)
+        o, tol, _, _ = AP.attend(wide[b * n_q:(b + 1) * n_q, 1:], k, v, [prefix + int(lens[b]) - n_q + i + 1 for i in range(n_q)], d ** -0.5)
+        _close(out[b * n_q:(b + 1) * n_q, 1:], o, tol)
+    assert bool((out[:, 0] == 7.0).all())
 
 
 @gpu
