@@ -101,17 +101,20 @@ __device__ __forceinline__ at_u32x2 at_tr_read(const uint16_t* __restrict__ p) {
   return __builtin_bit_cast(at_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_tr_ptr)p));
 }
 
-// The wait states between a matrix product and the first read of its result, which the compiler counts and fills.
-// Where two ways lead from the one to the other, of which the first that it follows is the longer and
+// The wait states between a matrix product and the first read of its result, which the compiler counts and
+// fills.  Where two ways lead from the one to the other, of which the first that it follows is the longer and
 // still shorter than the wait, it does not count the other (a short branch between them: scores that were read
-// too early, here).  So they are spent in front of such branches: 11 states of a 16 x 16 product, 18
-// of a 32 x 32.
-// at_products_done(x) after the last product, x its result; at_products_with(y) behind it holds back the reads of
-// earlier ones.
-__device__ __forceinline__ void at_products_done(at_f32x4& x) { asm volatile("s_nop 7\n\ts_nop 2" : "+v"(x)); }
-__device__ __forceinline__ void at_products_done(at_f32x16& x) { asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 1" : "+v"(x)); }
-
-template <class T> __device__ __forceinline__ void at_products_with(T& y) { asm volatile("" : "+v"(y)); }
+// too early, here).  So they are spent in front of such branches: 11 states of a 16 x 16 x 32 product, and as
+// many of a 32 x 32 x 16.  The empty statements keep every product of x in front of the wait and every read
+// of its results behind.
+template <class T, int N>
+__device__ __forceinline__ void at_products_done(T (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+  asm volatile("s_nop 7\n\ts_nop 2");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
 
 // A row's weights are taken relative to a maximum that may lag behind by up to 2^AT_LAG: the
 // accumulated sums are rescaled only when some row of the wave passes it.  Weights up to 2^8

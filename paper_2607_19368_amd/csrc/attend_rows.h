@@ -220,9 +220,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
 #pragma unroll
       for (int n = 0; n < NR; ++n) s[n] = TY::mfma16(kf, qf[n][st], s[n]);
     }
-    at_products_done(s[NR - 1]);
-#pragma unroll
-    for (int n = 0; n + 1 < NR; ++n) at_products_with(s[n]);
+    at_products_done(s);
     at_u32x2 pf[NR];                               // P^T: keys 4 grp + 0..3
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
@@ -277,11 +275,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
   }
 
   // the waves join
-  at_products_done(o[NR - 1][DB - 1]);
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-#pragma unroll
-    for (int b = 0; b < DB; ++b) at_products_with(o[n][b]);
+    at_products_done(o[n]);
     const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[n]), __float_as_uint(l[n]), false, false);
     l[n] = __uint_as_float(w32[0]) + __uint_as_float(w32[1]);
     const auto w16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(l[n]), __float_as_uint(l[n]), false, false);

@@ -209,7 +209,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
       if (next >= 0) load_tile(next, nbuf);
       scores(std::false_type{}, s, ck, nullptr, nullptr, nbuf);
     }
-    // (see at_products_done: of the ways past this branch the one through it is long enough by itself)
+    // (see at_products_done: of the ways past this branch the longer is long enough by itself)
     if (masked) {
       int left = limit - j0 - 4 * half;
       asm volatile("" : "+v"(left));               // a branch, not 32 selects in every tile
@@ -344,9 +344,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     find_pages(min(tile + 2, t1 - 1));
   }
 
-  at_products_done(o[DB - 1]);
-#pragma unroll
-  for (int b = 0; b + 1 < DB; ++b) at_products_with(o[b]);
+  at_products_done(o);
   {
     const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(w[0]) + __uint_as_float(w[1]);

@@ -294,6 +294,22 @@ def test_attend_again_gives_the_same_bits(dt, d):
 
 
 @gpu
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+def test_paged_again_gives_the_same_bits(dt, d):
+    g = _gen(d)
+    for B_, n_q, Hq, Hkv, prefix in ((3, 1, 14, 2, 90), (3, 3, 14, 2, 90), (40, 3, 14, 2, 2000), (40, 1, 14, 2, 2000), (5, 5, 28, 1, 300)):
+        pages = -(-prefix // 16)
+        kc, vc = (torch.randn(pages + B_ * 9, Hkv, 16, d, generator=g).to(dt).cuda() for _ in range(2))
+        table = (pages + torch.arange(B_ * 9, dtype=torch.int32)).view(B_, 9).cuda()
+        lens = torch.randint(n_q, 145, (B_,), generator=g).int().cuda()
+        q = torch.randn(B_, n_q, Hq, d, generator=g).to(dt).cuda()
+        pre = torch.arange(pages, dtype=torch.int32).cuda()
+        want = P.slh_attend_paged(q, kc, vc, table, lens, pre, prefix)
+        assert all(torch.equal(P.slh_attend_paged(q, kc, vc, table, lens, pre, prefix), want) for _ in range(4))
+
+
+@gpu
 def test_attend_on_another_stream_and_in_a_graph():
     g = _gen(8)
     n = 200
