@@ -17,12 +17,13 @@ _HALVES = (torch.bfloat16, torch.float16)
 # singletons, devices are compared by index, and the stream is asked for as an integer.
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call(name, dev, stream, args):
     """Calls the library's function `name` on device `dev` with args and the stream."""
     f = getattr(B.load(), name)
-    if torch.cuda.current_device() == dev:
+    if _current_device() == dev:
         rc = f(*args, _current_stream(dev) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(dev):
@@ -167,7 +168,7 @@ def _workspace(need, dev, workspace, device, stream):
 def _bytes(name, dev, args):
     """What a workspace function says for device `dev`."""
     f = getattr(B.load(), name)
-    if torch.cuda.current_device() == dev:
+    if _current_device() == dev:
         return f(*args)
     with torch.cuda.device(dev):
         return f(*args)
