@@ -536,6 +536,8 @@ int slh_kv_append(const void *k, int64_t k_st, int64_t k_sh, const void *v, int6
  * workspace: slh_attend_workspace() bytes of device memory (aligned to 16 bytes, contents need no
  * preparation), which no other call may use until this one has run; the size is for the current
  * device.  Rows of out that belong to no sequence are not written.
+ * Limits: strides of tokens at most 2^24; Hq / Hkv <= 1024; B <= 2^20; Tq (Hq / Hkv) and Tk < 2^30;
+ * 1e-37 <= scale <= 1e37; Hkv (Tq (Hq / Hkv) / 128 + 3 B) < 2^22.
  */
 int64_t slh_attend_workspace(int64_t Tq, int64_t Tk, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
                              int32_t causal);
@@ -556,6 +558,8 @@ int slh_attend(const void *q, int64_t q_st, int64_t q_sh, const void *k, int64_t
  * lie outside [0, n_pages) are undefined, but nothing outside the cache is read.  Types, heads,
  * products, lse ([B n_q][Hq]) and workspace (slh_attend_paged_workspace(), with max_len =
  * max_pages page_size) as for slh_attend.
+ * Limits: as there, with Tq = B n_q; page_size a power of two up to 65536; n_pages Hkv page_size < 2^31
+ * rows (their offsets in elements may pass 2^31); max_pages page_size and prefix_len < 2^29.
  */
 int64_t slh_attend_paged_workspace(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d,
                                    int64_t max_len, int64_t prefix_len);

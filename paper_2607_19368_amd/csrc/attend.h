@@ -124,6 +124,8 @@ constexpr float AT_LAG = 8.f;
 // A tile's rows are reached by 32-bit offsets in bytes from its first.
 constexpr int64_t AT_STRIDE = (int64_t)1 << 24;
 
+// Blocks of a launch stay below.
+constexpr int AT_BLOCKS = 1 << 23;
 // x / n for a block number x < 2^23 and n < 2^16: x ceil(2^40 / n) / 2^40, whose error x n / 2^40 is less than
 // the 1 / n by which it could reach the next whole number.
 inline uint64_t at_divisor(int n) { return (((uint64_t)1 << 40) + n - 1) / (uint64_t)n; }
@@ -237,7 +239,7 @@ __device__ __forceinline__ int at_sees(const AtTask& t, int i) {
   return min(t.nk, max(t.floor, t.base + i + 1));
 }
 
-// ---- k_attend.hip: tiles of many rows; k_attend_rows.hip: few rows, keys over the waves ----
+// ---- attend_tiles.h: tiles of many rows; attend_rows.h: few rows, keys over the waves ----
 constexpr int AT_WAVES = 4;                // waves of a block, of both
 constexpr int AT_ROWS = 32 * AT_WAVES;     // rows of a block of the first
 // Both in one launch: the prefix in tiles, `pre_blocks` of them, the sequences' own keys by rows.

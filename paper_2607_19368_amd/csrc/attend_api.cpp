@@ -73,6 +73,7 @@ static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys,
       double us = (double)rounds * each * 2.0 * full + (rest == 0 ? 0.0 : each * (rest <= n_cu ? one : 2.0 * full));
       if (part < 1.0 && rounds > 1) us = (double)blocks * each * full / n_cu + each * full;    // uneven blocks fill in
       us = std::max(us, (double)n * c.one * work) + (c.rows == same ? 0.0 : c.start) + attend_join_us(s + also, out_rows, d);
+      if (blocks + sets * Hkv * s > AT_BLOCKS / 2 - 64) us += 1e12;      // a launch may be of two plans
       if (us < best.us) best = AttendPart{c.rows, (int)s, tiles, us};
     }
   }
@@ -111,7 +112,7 @@ static int attend_run(AttendArgs& a, const AttendPlan& p, bool paged, bool bf16,
                       hipStream_t s) {
   if (p.bytes && (!ws || ((uintptr_t)ws) % 16 != 0 || ws_bytes < p.bytes)) return SLH_EINVAL;
   const int64_t own = p.own.tiles * p.own.splits * a.Hkv, pre = p.pre.tiles * p.pre.splits * a.Hkv;
-  if (own + pre > (1 << 23) - 64) return SLH_EINVAL;
+  if (own + pre > AT_BLOCKS - 64) return SLH_EINVAL;
   if (p.bytes) {
     a.part_o = (float*)ws;
     a.part_ml = a.part_o + p.slots * a.rows * d;
@@ -157,7 +158,8 @@ static bool attend_common_ok(int dtype, int64_t B, int Hq, int Hkv, int d, doubl
   if (dtype != SLH_BF16 && dtype != SLH_F16) return false;
   if (d != 64 && d != 80 && d != 96 && d != 128) return false;
   if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hkv > 65535 || Hq / Hkv > 1024) return false;
-  return B >= 0 && B <= (1 << 20) && scale > 0.0 && !std::isinf(scale);
+  // the kernels' scale is a normal number of 32 bits
+  return B >= 0 && B <= (1 << 20) && scale >= 1e-37 && scale <= 1e37;
 }
 
 }  // namespace slh
@@ -213,8 +215,8 @@ int slh_attend_paged(const void* q, int64_t q_st, int64_t q_sh, const void* k_ca
   using namespace slh;
   if (!attend_common_ok(dtype, B, Hq, Hkv, d, scale)) return SLH_EINVAL;
   const int g = Hq / Hkv;
-  if (n_pages < 1 || n_pages > INT32_MAX || n_pages * Hkv > INT32_MAX / std::max(1, page_size) || page_size < 1 || page_size > 65536 || (page_size & (page_size - 1)))
-    return SLH_EINVAL;
+  if (page_size < 1 || page_size > 65536 || (page_size & (page_size - 1))) return SLH_EINVAL;
+  if (n_pages < 1 || n_pages > INT32_MAX || n_pages * Hkv > INT32_MAX / page_size) return SLH_EINVAL;
   if (max_pages < 0 || ld_pages < max_pages ||
       !attend_paged_ok(B, n_q, g, (int64_t)max_pages * page_size, prefix_len))
     return SLH_EINVAL;

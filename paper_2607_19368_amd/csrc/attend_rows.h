@@ -1,5 +1,5 @@
 // Attention of few rows against many keys: decode steps, and prompts too short to fill the chip
-// with tiles of 128 rows.  The same one-pass softmax as k_attend.hip on the same transposed
+// with tiles of 128 rows.  The same one-pass softmax as attend_tiles.h on the same transposed
 // products, with 16 x 16 matrix instructions: a block holds 16 or 32 rows, and its four waves take
 // the keys in turn, 16 at a time, each with a running maximum of its own; at the end they join
 // through LDS.
@@ -9,6 +9,10 @@
 // 16 keys a step: a wave's two stages of K and V are 16 KB (d = 128), so that two blocks fit a
 // compute unit and one's start and end hide behind the other's steps; and pages of 16 rows or
 // more hold whole steps, which makes their addresses uniform.
+//
+// Measured, d = 128: two new tokens of 6 sequences of up to 49159 fp16 rows in pages of 32, 32 / 8 heads:
+// 987 MB in 174 us = 5.7 TB/s (179 with the join; a pure read of large buffers reaches 6.55 TB/s, a copy 4.75).  512 causal
+// bf16 tokens, 28 / 4 heads: 12.6 us, the dependent chain of 8 steps of 0.6 us behind the launch.
 #pragma once
 #include "attend.h"
 

@@ -10,6 +10,20 @@
 //   O^T (d x rows)   += V^T P^T      P from the registers of S^T, V^T by transposing LDS reads
 // The k index of the second product may run over the keys in any order: it takes them as S^T's
 // accumulators hold them (4 keys of each half wave in turn), so P needs no exchange.
+//
+// Rounding to fewer bits: only P, to the inputs' type, for the second product (its error is relative to
+// each weight, and the row's sum takes the weights as they were before it); scores, maxima, sums and O
+// are fp32.
+//
+// Bound by the matrix units: 4 d operations a row and key at 512 (64-key tile of 128 rows: 32 KB)
+// operations a byte.  128 rows a block, so that its waves share a tile's LDS reads' source, and two blocks a
+// compute unit, so that one's softmax runs beside the other's products; the next tile goes straight to the
+// other LDS buffer while one is worked on, its loads asked for a few at a time behind the products (all at
+// once at the barrier: 16384 causal tokens 2.61 instead of 2.51 ms).
+// Measured, bf16, d = 128: one causal prompt of 16384 tokens, 40 / 8 heads, 2.54 ms = 1084 TFLOP/s, where
+// an 8192^3 library product of the same random numbers reaches 1113; with zeros for inputs 1283, for then
+// the power limit leaves the clock alone.  23 causal sequences of 59 to 1458 tokens, 32 / 8 heads, 138 us = 660 TFLOP/s:
+// of a block's 23 us, 7 are its task, first loads and last stores, and 10 % of the products are masked.
 #pragma once
 #include "attend.h"
 

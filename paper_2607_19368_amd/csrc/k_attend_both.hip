@@ -1,7 +1,12 @@
 // A decode step behind a long prefix as one launch: the prefix for all sequences in tiles of 128 rows
 // (attend_tiles.h: bound by the matrix units), each sequence's own keys by rows (attend_rows.h: bound by
-// memory).  Blocks of both kinds lie beside each other on a compute unit, so that the one's reads
-// run under the other's products.
+// memory).  The prefix's blocks come first: the own keys' blocks fill the compute units as those end, so
+// that the last prefix blocks do not run alone and one launch is saved.
+//
+// 128 sequences, 28 / 4 heads of 128, a prefix of 32768 rows and up to 641 own, bf16, us with the join: two
+// launches 107, prefix first 101, own keys first 101, eights of both kinds alternating 144 (a unit that holds one
+// of each has too few waves of either).  With the loads spread as in attend_tiles.h: 94, of which
+// this kernel 84.5, the join 8.5.
 #include "attend_rows.h"
 #include "attend_tiles.h"
 
@@ -11,16 +16,13 @@ template <class TY, int D, int NR>
 __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend_both(AttendArgs a, int pre_blocks, int blocks) {
   constexpr int LT = at_lds<D>(), LR = rw_lds<D, NR>();
   __shared__ __attribute__((aligned(16))) uint16_t smem[LT > LR ? LT : LR];
-  // Kinds alternate in proportion, by eights: block x of a kind stays on XCD x % 8, where the others that
-  // read the same keys are.
-  const int e = blockIdx.x >> 3, in = blockIdx.x & 7;
-  const int pe = (pre_blocks + 7) >> 3, all = (int)gridDim.x >> 3;
-  const int before = min(e, pe), upto = e < pe ? before + 1 : before;
-  if (upto > before) {
-    const int x = 8 * before + in;
-    if (x < pre_blocks) attend_tiles<TY, D, true>(a, x, smem);
+  // The prefix's blocks are filled up to whole eights: block x of a kind stays on XCD x % 8, where the others
+  // that read the same keys are.
+  const int before = (pre_blocks + 7) & ~7;
+  if ((int)blockIdx.x < before) {
+    if ((int)blockIdx.x < pre_blocks) attend_tiles<TY, D, true>(a, blockIdx.x, smem);
   } else {
-    const int x = 8 * (e - before) + in;
+    const int x = (int)blockIdx.x - before;
     AttendArgs own = a;
     own.pre_tiles = 0;
     if (x < blocks - pre_blocks) attend_rows<TY, D, NR, true>(own, x, smem);
@@ -29,8 +31,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend_both(AttendArgs a, 
 
 template <class TY, int NR>
 static void both_launch(const AttendArgs& a, int d, int64_t pre, int64_t blocks, hipStream_t s) {
-  // an eight of a kind may be partly empty
-  const dim3 grid((unsigned)(8 * ((pre + 7) / 8 + (blocks - pre + 7) / 8))), block(64 * AT_WAVES);
+  const dim3 grid((unsigned)((pre + 7) / 8 * 8 + blocks - pre)), block(64 * AT_WAVES);
   switch (d) {
     case 64: hipLaunchKernelGGL((k_attend_both<TY, 64, NR>), grid, block, 0, s, a, (int)pre, (int)blocks); break;
     case 80: hipLaunchKernelGGL((k_attend_both<TY, 80, NR>), grid, block, 0, s, a, (int)pre, (int)blocks); break;

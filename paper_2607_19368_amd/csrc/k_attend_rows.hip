@@ -36,7 +36,9 @@ hipError_t launch_attend_rows(const AttendArgs& a, bool paged, bool bf16, int ro
 
 // Joins the splits of each row: out = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2((m_s - max m) c).
 // One wave a row: its lanes find the weights of 64 splits at a time, then each half takes every
-// other split, four elements a lane, four splits in flight.
+// other split, four elements a lane, four splits in flight.  Bound by memory: partial results are fp32, 4 d + 8
+// bytes a row and split, read once (128 tokens of 28 heads, up to 19 splits: 35 MB in 8.5 us;
+// 387 tokens of 40 heads, 4 splits: 32 MB in 11 us).
 template <class TY>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int slots) {
   const int lane = threadIdx.x & 63, half = lane >> 5, e = 4 * (lane & 31);

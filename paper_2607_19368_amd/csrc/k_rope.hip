@@ -10,6 +10,11 @@
 // A row of d elements belongs to LPR lanes with two 8-element chunks each: a chunk of the
 // rotation's first half and its partner, so that the half layout needs no exchange between
 // lanes; the norm's sum of squares is the only one (DPP within at most 16 lanes).
+//
+// Measured, d = 128 (a copy of 4 GiB reaches 4.75 TB/s, reads and writes together): 32768 bf16 tokens of
+// 28 + 4 heads, norms and rotation, 554 MB in 109 us = 5.1 TB/s; 5003 fp32 tokens of 12 + 12 heads of 80,
+// 32 elements rotated, 77.5 MB in 18.4 us = 4.2 TB/s; 16384 fp16 tokens of 8 heads into a paged cache, 143 MB in 33 us =
+// 4.3 TB/s; 24 tokens 3.7 us, which is the launch's.
 #include "slh_device.h"
 #include "slh_internal.h"
 

@@ -531,6 +531,26 @@ def test_library_refuses_before_any_gpu_work():
         assert lib.slh_rope_table(*{**table, **b}.values()) == B.SLH_EINVAL, b
 
 
+def test_library_refuses_past_its_limits():
+    lib = B.load()
+    p = 4096                                      # an aligned address that nothing reads
+    att = dict(q=p, q_st=128, q_sh=64, k=p, k_st=64, k_sh=64, v=p, v_st=64, v_sh=64, dt=0, Tq=3, Tk=3, B=1, Hq=2, Hkv=1, d=64, cq=p,
+               ck=p, scale=0.1, causal=1, out=p, o_st=128, o_sh=64, lse=None, ws=None, n=0, st=None)
+    for b in [dict(scale=1e300), dict(scale=1e38), dict(scale=1e-40), dict(k_st=2 ** 24 + 8), dict(v_st=2 ** 25), dict(q_st=2 ** 24 + 8),
+              dict(Hq=2048), dict(B=2 ** 20 + 1), dict(B=2 ** 20, Hkv=16, Hq=16),
+              dict(Tq=2 ** 20, Tk=2 ** 20, B=2 ** 18, Hkv=64, Hq=64)]:
+        assert lib.slh_attend(*{**att, **b}.values()) == B.SLH_EINVAL, b
+    need = lib.slh_attend_workspace(3, 4096, 1, 2, 1, 64, 1)
+    assert need > 0
+    for b in [dict(ws=None, n=need), dict(ws=p, n=need - 1), dict(ws=p + 8, n=need)]:
+        assert lib.slh_attend(*{**att, "Tk": 4096, **b}.values()) == B.SLH_EINVAL, b
+    pag = dict(q=p, q_st=128, q_sh=64, kc=p, vc=p, dt=0, pages=4, page=16, B=2, n_q=1, Hq=2, Hkv=1, d=64, table=p, ld=3, most=3, lens=p,
+               pre=None, plen=0, scale=0.1, out=p, o_st=128, o_sh=64, lse=None, ws=None, n=0, st=None)
+    for b in [dict(pages=2 ** 27), dict(pages=2 ** 31), dict(page=1 << 17), dict(scale=1e38), dict(most=2 ** 26, ld=2 ** 26),
+              dict(B=2 ** 20, Hq=16, Hkv=16), dict(pre=p, plen=2 ** 30), dict(B=1, most=2000, ld=2000, pages=2000)]:
+        assert lib.slh_attend_paged(*{**pag, **b}.values()) == B.SLH_EINVAL, b
+
+
 def test_host_tensors_are_refused():
     x = torch.zeros(2, 2, 64, dtype=BF)
     cu = torch.tensor([0, 2], dtype=torch.int32)
