@@ -244,7 +244,7 @@ constexpr int AT_WAVES = 4;                // waves of a block, of both
 constexpr int AT_ROWS = 32 * AT_WAVES;     // rows of a block of the first
 // Both in one launch: the prefix in tiles, `pre_blocks` of them, the sequences' own keys by rows.
 // d, paged, bf16 and rows (16 or 32) pick the instantiation; `blocks` as the tasks need.
-hipError_t launch_attend_tiles(const AttendArgs& a, bool paged, bool bf16, int d, int64_t blocks, hipStream_t s);
+hipError_t launch_attend_tiles(const AttendArgs& a, bool paged, bool bf16, int rows, int d, int64_t blocks, hipStream_t s);
 hipError_t launch_attend_rows(const AttendArgs& a, bool paged, bool bf16, int rows, int d, int64_t blocks, hipStream_t s);
 hipError_t launch_attend_both(const AttendArgs& a, bool bf16, int rows, int d, int64_t pre_blocks, int64_t blocks,
                               hipStream_t s);

@@ -23,7 +23,7 @@ static int attend_cus() {
 
 // Which kernel takes a set of rows, in how many pieces of its keys.
 struct AttendPart {
-  int rows;               // of a block: AT_ROWS (k_attend), 32 or 16 (k_attend_rows)
+  int rows;               // of a block: AT_ROWS or half of it (k_attend), 32 or 16 (k_attend_rows)
   int splits;
   int64_t tiles;          // row tiles of a key/value head, all sequences together
   double us;
@@ -36,43 +36,67 @@ struct AttendPlan {
 
 // What a launch costs, in microseconds, as measured with d = 128 on 256 compute units.  A block goes
 // through its keys 64 at a time: a tile of k_attend, or a step of each wave of k_attend_rows.  `start`:
-// of the launch, of finding rows and keys, of the first loads and the last stores; `one`: a block's 64
-// keys where it has a compute unit nearly to itself; `full`: a unit's 64 keys of one block, two
-// resident.  Measured against it, graph replays, us (model in brackets):
-//   queries x context, heads     16 rows        32 rows       128 rows
-//   512 x 0, 28 / 4              16.3 (16)      13.0 (13)     17 (17)
-//   1024 x 0, 28 / 4             37.2 (37)      28.7 (29)     27 (27)
-//   16 x 16384, 28 / 4           30.0           34.6 (31)     22.5 (24)
-//   1 x 32768, 28 / 4            22.9           24.7          25.7
-struct AttendCost { int rows; double start, one, full; };
-static const AttendCost ATTEND_COSTS[3] = {{16, 6.5, 0.65, 0.52}, {32, 7.0, 0.75, 0.72}, {AT_ROWS, 6.5, 1.3, 1.05}};
-// Partial results: two more passes over memory, and a launch.
+// of a block, for finding its rows and keys, its first loads and its last stores (and ATTEND_LAUNCH of the launch);
+// `one`: a block's 64 keys where it has a compute unit to itself; `pair`: where another block is beside
+// it; `full`: a unit's 64 keys of one block with all units busy for several rounds (power and caches are shared then).
+// Over 53 packed shapes (16 to 10000 tokens, 0 to 9000 keys in front) the plan's time is on average 1.02 of the best
+// of all kernels and 1 to 32 splits, over 45 paged ones 1.03.  One split, us, queries x context, heads:
+//                            16 rows   32 rows   64 rows   128 rows
+//   256 x 0, 28 / 4            7.3       9.0       8.8      10.4
+//   512 x 0, 28 / 4           15.3      12.7      12.3      15.4
+//   1024 x 0, 28 / 4                    29.6      21.8      25.2
+//   1024 x 2000, 40 / 8                 112       82.0      76.0
+//   3000 x 0, 28 / 4                    136       88.7      80.9
+struct AttendCost { int rows; double start, one, pair, full; };
+static const AttendCost ATTEND_COSTS[4] = {
+    {16, 1.8, 0.65, 0.8, 0.33}, {32, 2.5, 0.75, 0.95, 0.42}, {AT_ROWS / 2, 2.6, 0.78, 1.1, 0.55}, {AT_ROWS, 3.0, 1.13, 1.75, 0.95}};
+static const double ATTEND_LAUNCH = 4.0;
+// Partial results: another pass over memory, the end of the blocks that write them, and a launch.
 static double attend_join_us(int64_t slots, int64_t rows, int d) {
-  return slots > 1 ? 4.0 + 2.0 * (double)(slots * rows) * (4.0 * d + 8.0) / 3.5e6 : 0.0;
+  return slots > 1 ? 3.0 + 0.1 * (double)slots + 1.35 * (double)(slots * rows) * (4.0 * d + 8.0) / 3.5e6 : 0.0;
 }
 
 // The kernel and the splits that cost least for `sets` runs of `rows` rows a key/value head against `keys` keys
 // each, of which a row tile sees `mean` on average.  out_rows: rows of a partial result.  also: other
 // partial results of a row; same: the kernel of a launch that this one would join.
-static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys, double mean, int64_t out_rows, int d, int n_cu,
-                              int also, int same) {
+static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys, double mean, int64_t out_rows,
+                              int d, int n_cu,
+                              int also, int same, bool paged) {
   AttendPart best = {};
   best.us = INFINITY;
   best.rows = 16, best.splits = 1;
-  const double work = d / 128.0, part = keys > 0 ? mean / (double)keys : 1.0;
+  // part of a block's time does not shrink with d: 4 heads of 64, 256 rows against 2256 keys, 0.79 us a tile of 128
+  // rows, 0.57 of 64, 0.52 of 32
+  const double work = 0.4 + 0.6 * d / 128.0, part = keys > 0 ? mean / (double)keys : 1.0;
   const int64_t units = (keys + 63) / 64, most = std::max<int64_t>(1, std::min<int64_t>(64, units)), slots = 2 * (int64_t)n_cu;
   for (const AttendCost& c : ATTEND_COSTS) {
+    if (paged && c.rows == AT_ROWS / 2) continue;
     const int64_t per = std::max<int64_t>(1, (rows + c.rows - 1) / c.rows), tiles = sets * per, base = tiles * Hkv;
     // a unit's 64 keys come from memory at 5.2 TB/s, once for the row tiles that share them
-    const double full = std::max(c.full * work, 256.0 * d * n_cu / 5.2e6 / (double)per), one = std::max(c.one * work, full);
+    const double mem = 256.0 * d * n_cu / 5.2e6 / (double)per;
+    const double full = std::max(c.full * work, mem), one = std::max(c.one * work, mem),
+                 pair = std::max(c.pair * work, 2.0 * mem);
     const int64_t fill = slots / std::max<int64_t>(1, base);
     for (const int64_t want : {(int64_t)1, (int64_t)2, (int64_t)3, fill / 2, fill, 2 * fill, 4 * fill, most}) {
       const int64_t s = std::max<int64_t>(1, std::min(want, most)), n = (units + s - 1) / s, blocks = base * s;
       const int64_t rounds = blocks / slots, rest = blocks - rounds * slots;
-      const double each = (double)n * part;
-      double us = (double)rounds * each * 2.0 * full + (rest == 0 ? 0.0 : each * (rest <= n_cu ? one : 2.0 * full));
-      if (part < 1.0 && rounds > 1) us = (double)blocks * each * full / n_cu + each * full;    // uneven blocks fill in
-      us = std::max(us, (double)n * c.one * work) + (c.rows == same ? 0.0 : c.start) + attend_join_us(s + also, out_rows, d);
+      const double each = (double)n * part, two = rounds > 1 || (rounds == 1 && rest) ? 2.0 * full : std::min(pair, 2.0 * full);
+      double us;
+      if (part < 1.0) {
+        // causal, the blocks with the most keys first, down to 2 part - 1 of the longest: the longest has one
+        // beside it for as long as the block takes that comes when all units have one, and all together take what
+        // the units can do
+        const double beside = blocks <= n_cu ? 0.0 : 1.0 - 2.0 * (1.0 - part) * n_cu / (double)blocks;
+        us = std::max((double)n * (beside * pair + (1.0 - beside) * one) + c.start,
+                      (double)blocks / n_cu * (each * two / 2.0 + c.start));
+        // nor do the last blocks, short as they are, start before whole rounds of the others have run
+        if (rounds && rest)
+          us = std::max(us, rounds * (each * two + 2.0 * c.start) +
+                        (2.0 * part - 1.0) * n * (rest <= n_cu ? one : two) + c.start);
+      } else {
+        us = (double)rounds * (each * two + 2.0 * c.start) + (rest == 0 ? 0.0 : each * (rest <= n_cu ? one : two) + c.start);
+      }
+      us += (same && (c.rows == same || c.rows == AT_ROWS) ? 0.0 : ATTEND_LAUNCH) + attend_join_us(s + also, out_rows, d);
       if (blocks + sets * Hkv * s > AT_BLOCKS / 2 - 64) us += 1e12;      // a launch may be of two plans
       if (us < best.us) best = AttendPart{c.rows, (int)s, tiles, us};
     }
@@ -90,7 +114,7 @@ static AttendPlan attend_plan_packed(int64_t Tq, int64_t Tk, int B, int Hq, int 
   // as if the sequences were equal; where they are not, their tiles are B more at most
   const int64_t rows = Tq * (Hq / Hkv), n = std::max(1, B), keys = Tk / n;
   const double mean = causal ? std::max((double)keys / 2, (double)keys - (double)Tq / n / 2) : (double)keys;
-  p.own = attend_part((rows + n - 1) / n, n, Hkv, keys, mean, Tq * Hq, d, attend_cus(), 0, 0);
+  p.own = attend_part((rows + n - 1) / n, n, Hkv, keys, mean, Tq * Hq, d, attend_cus(), 0, 0, false);
   p.own.tiles = rows / p.own.rows + B;
   attend_finish(p, Tq * Hq, d);
   return p;
@@ -100,9 +124,9 @@ static AttendPlan attend_plan_paged(int B, int n_q, int Hq, int Hkv, int d, int6
   AttendPlan p = {};
   const int n_cu = attend_cus();
   const int64_t rows = (int64_t)n_q * (Hq / Hkv), out_rows = (int64_t)B * n_q * Hq;
-  p.own = attend_part(rows, B, Hkv, max_len, (double)max_len, out_rows, d, n_cu, prefix_len > 0, 0);
+  p.own = attend_part(rows, B, Hkv, max_len, (double)max_len, out_rows, d, n_cu, prefix_len > 0, 0, true);
   if (prefix_len > 0)
-    p.pre = attend_part(B * rows, 1, Hkv, prefix_len, (double)prefix_len, out_rows, d, n_cu, p.own.splits, p.own.rows);
+    p.pre = attend_part(B * rows, 1, Hkv, prefix_len, (double)prefix_len, out_rows, d, n_cu, p.own.splits, p.own.rows, true);
   attend_finish(p, out_rows, d);
   return p;
 }
@@ -123,8 +147,8 @@ static int attend_run(AttendArgs& a, const AttendPlan& p, bool paged, bool bf16,
   a.by_splits = at_divisor(a.splits);
   a.by_pre_splits = at_divisor(std::max(1, a.pre_splits));
   auto go = [&](int rows, int64_t blocks) {
-    return rows == AT_ROWS ? launch_attend_tiles(a, paged, bf16, d, blocks, s)
-                           : launch_attend_rows(a, paged, bf16, rows, d, blocks, s);
+    return rows >= AT_ROWS / 2 ? launch_attend_tiles(a, paged, bf16, rows, d, blocks, s)
+                               : launch_attend_rows(a, paged, bf16, rows, d, blocks, s);
   };
   (void)hipGetLastError();
   a.pre_tiles = (int)p.pre.tiles;

@@ -11,6 +11,12 @@
 // The k index of the second product may run over the keys in any order: it takes them as S^T's
 // accumulators hold them (4 keys of each half wave in turn), so P needs no exchange.
 //
+// KW: 1, a block holds 128 rows, 32 a wave.  2, where so few blocks would leave compute units idle: 64 rows, and
+// of each tile's 64 keys two waves take the first half, two the second, with maxima and sums of
+// their own that are joined through LDS at the end.  A block's tile then takes 0.78 instead of 1.13 us, and
+// there are twice as many (KW 2 / KW 1, us, causal prompts: 512 tokens, 28 / 4 heads 12.3 / 15.4; 1024: 21.8 / 25.2;
+// 2048: 44.7 / 51.9; 3000: 88.7 / 80.9; 4096: 147 / 122: all units busy, K and V are read twice as often).
+//
 // Rounding to fewer bits: only P, to the inputs' type, for the second product (its error is relative to
 // each weight, and the row's sum takes the weights as they were before it); scores, maxima, sums and O
 // are fp32.
@@ -58,11 +64,13 @@ __device__ __forceinline__ void at_tile_barrier() {
 template <int D> constexpr int at_lds_tile() { return AT_KEYS * D + 64; }
 template <int D> constexpr int at_lds() { return 4 * at_lds_tile<D>() + 2 * AT_WAVES; }
 
-template <class TY, int D, bool PAGED>
+template <class TY, int D, bool PAGED, int KW>
 __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uint16_t* smem) {
   constexpr int CH = D / 8;                        // 16-byte chunks of a row
   constexpr int KS = D / 16;                       // k steps of K Q^T
   constexpr int DB = (D + 31) / 32;                // 32-row blocks of O^T
+  constexpr int ROWS = AT_ROWS / KW;
+  constexpr int NB = 2 / KW;                       // 32-key blocks of a tile that a wave takes
   constexpr int NL = AT_KEYS * CH / 64;            // 1 KB direct-to-LDS loads of a tile of K or V
   constexpr int LDX = (NL + AT_WAVES - 1) / AT_WAVES;
   uint16_t* const sK = smem;                       // [2][at_lds_tile]
@@ -73,17 +81,18 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   AtTask t;
   int kvh;
-  if (!at_task<PAGED, AT_ROWS>(a, block, t, kvh)) return;
+  if (!at_task<PAGED, ROWS>(a, block, t, kvh)) return;
 
   // this lane's row: token i of the run, head kvh g + h
-  const int row = t.r0 + 32 * wave + (lane & 31);
+  const int rw = KW == 1 ? wave : wave % (AT_WAVES / KW), kw = KW == 1 ? 0 : wave / (AT_WAVES / KW);
+  const int row = t.r0 + 32 * rw + (lane & 31);
   const bool real = row < t.r1;
   const int rr = real ? row : t.r1 - 1;
   const int i = rr / a.g, h = kvh * a.g + rr - i * a.g;
   const int limit = at_sees(t, i);
   // the most keys that a row of the block sees, and the fewest that one of the wave does
   const int end = max(0, at_sees(t, (t.r1 - 1) / a.g));
-  const int least = __builtin_amdgcn_readfirstlane(at_sees(t, min(t.r0 + 32 * wave, t.r1 - 1) / a.g));
+  const int least = __builtin_amdgcn_readfirstlane(at_sees(t, min(t.r0 + 32 * rw, t.r1 - 1) / a.g));
   // tiles of this split
   const int all = (end + AT_KEYS - 1) / AT_KEYS, each = (all + t.n_split - 1) / t.n_split;
   const int t0 = min(all, t.split * each), t1 = min(all, t0 + each);
@@ -174,7 +183,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
   // V^T: lane's element of a 32 x 16 block: row d = lane & 31, keys 4 half + 0..3 and 8 + those
   const int i16 = lane & 15, hi = (lane >> 4) & 1;
   auto v_read = [&](const uint16_t* cv, int b, int kc, int e) {
-    const int r = 16 * kc + 8 * e + 4 * half + i16 / 4;
+    const int r = 32 * NB * kw + 16 * kc + 8 * e + 4 * half + i16 / 4;
     const int ch = 4 * b + 2 * hi + (i16 % 4) / 2;
     return at_tr_read(cv + r * D + 8 * (ch ^ at_vswz<D>(r)) + 4 * (i16 & 1));
   };
@@ -183,13 +192,13 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
   // ahead they would take the registers that O needs.  LOADS: the next tile's (even) loads go out a
   // few behind each step's products.  The block's waves meet at the same point of each tile, and sent in
   // one go their loads would hold every wave up for about 880 cycles of a tile's 3700.
-  auto scores = [&](auto loads, at_f32x16 (&s)[2], const uint16_t* ck, const uint16_t* kt, const uint16_t* vt, int nbuf)
+  auto scores = [&](auto loads, at_f32x16 (&s)[NB], const uint16_t* ck, const uint16_t* kt, const uint16_t* vt, int nbuf)
       __attribute__((always_inline)) {
-    at_u32x4 kf[2][2];
+    at_u32x4 kf[2][NB];
     auto k_read = [&](int st) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const int r = 32 * kb + (lane & 31);
+      for (int kb = 0; kb < NB; ++kb) {
+        const int r = 32 * (NB * kw + kb) + (lane & 31);
         kf[st & 1][kb] = *(const at_u32x4*)(ck + r * D + 8 * ((2 * st + half) ^ at_kswz<D>(r)));
       }
     };
@@ -199,7 +208,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     for (int st = 0; st < KS; ++st) {
       if (st + 1 < KS) k_read(st + 1);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) s[kb] = TY::mfma(kf[st & 1][kb], qf[st], s[kb]);
+      for (int kb = 0; kb < NB; ++kb) s[kb] = TY::mfma(kf[st & 1][kb], qf[st], s[kb]);
       if (decltype(loads)::value) {
 #pragma unroll
         for (int c = st * 2 * LDX / KS; c < (st + 1) * 2 * LDX / KS; ++c) load_even(kt, vt, nbuf, c);
@@ -212,9 +221,9 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
   // One tile.  masked: some row of the wave does not see all of its keys.  next: the tile to load meanwhile, -1:
   // none.
   auto tile_step = [&](bool masked, const uint16_t* ck, const uint16_t* cv, int j0, int next, int nbuf) {
-    at_f32x16 s[2];
+    at_f32x16 s[NB];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
     if (next >= 0 && is_even(next)) {
@@ -225,17 +234,17 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     }
     // (see at_products_done: of the ways past this branch the longer is long enough by itself)
     if (masked) {
-      int left = limit - j0 - 4 * half;
+      int left = limit - j0 - 32 * NB * kw - 4 * half;
       asm volatile("" : "+v"(left));               // a branch, not 32 selects in every tile
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (32 * kb + 8 * (e / 4) + e % 4 >= left) s[kb][e] = -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
     {
@@ -257,15 +266,15 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     if (a.c > 1.f) {
       // the largest scores times c are past fp32: the maximum leaves them first
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[kb][e] -= at;
       mu = 0.f;
     }
     float sum0 = 0.f, sum1 = 0.f;
-    at_u32x4 pf[4];                                // P^T, 16 keys each
+    at_u32x4 pf[2 * NB];                                // P^T, 16 keys each
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][e], a.c, -mu));
@@ -287,8 +296,8 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     v_step(0);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int kc = 0; kc < 4; ++kc) {
-      if (kc < 3) v_step(kc + 1);
+    for (int kc = 0; kc < 2 * NB; ++kc) {
+      if (kc + 1 < 2 * NB) v_step(kc + 1);
 #pragma unroll
       for (int b = 0; b < DB; ++b) o[b] = TY::mfma(vf[kc & 1][b], pf[kc], o[b]);
       __builtin_amdgcn_sched_barrier(0);
@@ -317,7 +326,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
 #pragma unroll
     for (int x = 0; x < AT_WAVES; ++x) any |= s_odd[x];
     if (__builtin_expect(!any, 1)) return;
-    for (int r = 0; r < AT_KEYS; ++r) {
+    for (int r = 32 * NB * kw; r < 32 * NB * (kw + 1); ++r) {
       if (j0 + r >= limit) continue;
 #pragma unroll
       for (int b = 0; b < DB; ++b)
@@ -362,6 +371,34 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
   {
     const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  }
+  if constexpr (KW == 2) {
+    // the waves that took the second half of each tile's keys give their sums to those of the first
+    __syncthreads();                               // every wave is done with its V
+    float* const so = (float*)smem + rw * (16 * DB + 2) * 64;
+    if (kw) {
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *(at_f32x4*)(so + (4 * b + e / 4) * 256 + 4 * lane) = at_f32x4{o[b][e], o[b][e + 1], o[b][e + 2], o[b][e + 3]};
+      so[16 * DB * 64 + lane] = m;
+      so[16 * DB * 64 + 64 + lane] = l;
+    }
+    __syncthreads();
+    if (kw) return;
+    const float m2 = so[16 * DB * 64 + lane], top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+    const float k1 = __builtin_amdgcn_exp2f((m - ref) * a.c), k2 = __builtin_amdgcn_exp2f((m2 - ref) * a.c);
+    m = top;
+    l = __builtin_fmaf(k1, l, k2 * so[16 * DB * 64 + 64 + lane]);
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const at_f32x4 x = *(const at_f32x4*)(so + (4 * b + e / 4) * 256 + 4 * lane);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) o[b][e + f] = __builtin_fmaf(k1, o[b][e + f], k2 * x[f]);
+      }
   }
   const bool empty = m == -INFINITY && l == 0.f;
   const int64_t r = (t.tok0 + i) * a.Hq + h;

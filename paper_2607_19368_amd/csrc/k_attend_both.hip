@@ -20,7 +20,7 @@ __global__ __launch_bounds__(64 * AT_WAVES, 2) void k_attend_both(AttendArgs a, 
   // that read the same keys are.
   const int before = (pre_blocks + 7) & ~7;
   if ((int)blockIdx.x < before) {
-    if ((int)blockIdx.x < pre_blocks) attend_tiles<TY, D, true>(a, blockIdx.x, smem);
+    if ((int)blockIdx.x < pre_blocks) attend_tiles<TY, D, true, 1>(a, blockIdx.x, smem);
   } else {
     const int x = (int)blockIdx.x - before;
     AttendArgs own = a;

@@ -35,14 +35,20 @@ hipError_t launch_attend_rows(const AttendArgs& a, bool paged, bool bf16, int ro
 }
 
 // Joins the splits of each row: out = sum_s w_s o_s / sum_s w_s l_s, w_s = exp2((m_s - max m) c).
-// One wave a row: its lanes find the weights of 64 splits at a time, then each half takes every
-// other split, four elements a lane, four splits in flight.  Bound by memory: partial results are fp32, 4 d + 8
+// WAVES waves a row: their lanes find the weights of 64 splits at a time, then the half waves take
+// the splits in turn, four elements a lane, four splits in flight.  One wave where there are many
+// rows; four where few rows of many splits would leave it to the latency of 16 loads after another (a
+// call with 28 rows, 64 splits: 18.2 instead of 21.8 us; 224 rows, 18 splits: 13.9, 15.4; 1280 rows: 26.9, 27.4;
+// 2048 rows: 41.3, 40.9).  Bound by memory: partial results are fp32, 4 d + 8
 // bytes a row and split, read once (128 tokens of 28 heads, up to 19 splits: 35 MB in 8.5 us;
 // 387 tokens of 40 heads, 4 splits: 32 MB in 11 us).
-template <class TY>
+template <class TY, int WAVES>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int slots) {
+  constexpr int PARTS = 2 * WAVES;                 // half waves of a row
+  __shared__ at_f32x4 s_o[WAVES == 1 ? 1 : WAVES * 32];
   const int lane = threadIdx.x & 63, half = lane >> 5, e = 4 * (lane & 31);
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int wave = threadIdx.x >> 6, part = WAVES == 1 ? half : 2 * wave + half;
+  const int64_t r = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   if (r >= a.rows) return;
   const int64_t tok = r / a.Hq;
   const int h = (int)(r - tok * a.Hq);
@@ -73,19 +79,19 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
     l += is_empty(v) ? 0.f : w * v.y;
     const unsigned long long there = __ballot(!is_empty(v));
     const int n = min(64, slots - s0);
-    for (int s = half; s < n + half; s += 8) {
+    for (int s1 = 0; s1 < n; s1 += 4 * PARTS) {
       at_f32x4 x[4];
       float ws[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int at = s + 2 * q;
+        const int at = s1 + part + PARTS * q;
         x[q] = at_f32x4{0.f, 0.f, 0.f, 0.f};
         ws[q] = __shfl(w, at & 63);
         if (at < n && ((there >> at) & 1) && e < d) x[q] = *(const at_f32x4*)(a.part_o + ((s0 + at) * a.rows + r) * d + e);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (s + 2 * q < n) {
+        if (s1 + part + PARTS * q < n) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) o[c] = __builtin_fmaf(ws[q], x[q][c], o[c]);
         }
@@ -95,6 +101,17 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
   for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
 #pragma unroll
   for (int c = 0; c < 4; ++c) o[c] += __shfl_xor(o[c], 32);
+  if constexpr (WAVES > 1) {
+    if (half == 0) s_o[32 * wave + lane] = o;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      const at_f32x4 x = s_o[32 * w + (lane & 31)];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] += x[c];
+    }
+  }
   const float inv = empty ? 0.f : 1.0f / l;
   if (half == 0 && e < d)
     *(at_u32x2*)(a.out + tok * a.o_st + h * a.o_sh + e) =
@@ -103,11 +120,16 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
 }
 
 hipError_t launch_attend_join(const AttendArgs& a, bool bf16, int d, int slots, hipStream_t s) {
-  const dim3 grid((unsigned)((a.rows + 3) / 4)), block(256);
-  if (bf16)
-    hipLaunchKernelGGL((k_attend_join<AtBf16>), grid, block, 0, s, a, d, slots);
+  const bool wide = slots > 8 && a.rows <= 1024;
+  const dim3 grid((unsigned)(wide ? a.rows : (a.rows + 3) / 4)), block(256);
+  if (bf16 && wide)
+    hipLaunchKernelGGL((k_attend_join<AtBf16, 4>), grid, block, 0, s, a, d, slots);
+  else if (bf16)
+    hipLaunchKernelGGL((k_attend_join<AtBf16, 1>), grid, block, 0, s, a, d, slots);
+  else if (wide)
+    hipLaunchKernelGGL((k_attend_join<AtF16, 4>), grid, block, 0, s, a, d, slots);
   else
-    hipLaunchKernelGGL((k_attend_join<AtF16>), grid, block, 0, s, a, d, slots);
+    hipLaunchKernelGGL((k_attend_join<AtF16, 1>), grid, block, 0, s, a, d, slots);
   return hipGetLastError();
 }
 

@@ -497,6 +497,67 @@ def test_paged_in_a_graph():
         assert torch.equal(out, P.slh_attend_paged(q, kc, vc, table, lens, pre, 100))
 
 
+# ---------------------------------------------------------------- blocks of 64 rows, joins of many splits
+@gpu
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_attend_prompts_between_few_and_many_rows(d, dt):
+    """Sizes between the kernels of few rows and of many: whole and ragged blocks, more keys than queries,
+    sequences of one token and of none."""
+    _attend_case([561], [561], 32, 4, d, dt, True, d)
+    _attend_case([257, 1, 0, 302], [257, 1, 3, 365], 32, 4, d, dt, True, d + 1)
+    _attend_case([190, 330], [201, 63], 32, 4, d, dt, False, d + 2)
+
+
+@gpu
+@pytest.mark.parametrize("lq,lk", [([60], [4001]), ([129, 31], [1500, 2000])])
+def test_attend_some_queries_many_keys(lq, lk):
+    _attend_case(lq, lk, 28, 4, 128, BF, True, len(lq))
+
+
+@gpu
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("at", [300, 351])         # in the first and the second half of a tile's keys
+def test_attend_values_not_seen_in_blocks_of_64_rows(dt, bad, at):
+    g = _gen(4)
+    n, d, Hq, Hkv = 560, 64, 32, 4
+    q, k, v = (torch.randn(n, h, d, generator=g).to(dt) for h in (Hq, Hkv, Hkv))
+    cu = torch.tensor([0, n], dtype=torch.int32).cuda()
+    clean = P.slh_attend(q.cuda(), k.cuda(), v.cuda(), cu).cpu()
+    v2 = v.clone()
+    v2[at, 2, 5] = bad
+    got = P.slh_attend(q.cuda(), k.cuda(), v2.cuda(), cu).cpu()
+    want = clean.clone()
+    want[at:, 16:24, 5] = bad
+    assert torch.equal(got.nan_to_num(nan=9.0), want.nan_to_num(nan=9.0))
+    k2 = k.clone()
+    k2[at, 2] = math.nan
+    got = P.slh_attend(q.cuda(), k2.cuda(), v.cuda(), cu).cpu()
+    want = clean.clone()
+    want[at:, 16:24] = math.nan
+    assert torch.equal(got.nan_to_num(nan=9.0), want.nan_to_num(nan=9.0))
+
+
+@gpu
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+def test_attend_blocks_of_64_rows_again_give_the_same_bits(dt, d):
+    g = _gen(d + 7)
+    cu = torch.tensor([0, 560, 1100], dtype=torch.int32).cuda()
+    q, k, v = (torch.randn(1100, h, d, generator=g).to(dt).cuda() for h in (28, 4, 4))
+    want = P.slh_attend(q, k, v, cu)
+    assert all(torch.equal(P.slh_attend(q, k, v, cu), want) for _ in range(4))
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 80, 128])
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_paged_many_splits_of_few_rows(d, dt):
+    _paged_case(1, 1, 7, 1, d, dt, 64, 2000, [3001], d)
+    _paged_case(2, 1, 4, 2, d, dt, 16, 0, [4100, 1], d + 1)
+
+
 # ---------------------------------------------------------------- refusals
 def test_library_refuses_before_any_gpu_work():
     lib = B.load()
