@@ -551,7 +551,7 @@ int slh_attend(const void *q, int64_t q_st, int64_t q_sh, const void *k, int64_t
  * The new tokens of a batch against a paged cache (as slh_kv_append writes it), behind a prefix that
  * every sequence shares: a decode step, or a few tokens at once.  Tokens b n_q <= t < (b + 1) n_q of
  * q and out are sequence b's.  Its keys are the prefix_len rows of prefix_pages (ceil(prefix_len /
- * page_size) entries; read once for all sequences) and lens[b] rows of its own pages, page_table[b
+ * page_size) entries; read once for all sequences, unless it is short) and lens[b] rows of its own pages, page_table[b
  * ld_pages + i] (max_pages entries), the n_q new tokens' own last among them: token i sees the
  * prefix and the first lens[b] - n_q + i + 1 own rows.  prefix_len 0: no prefix.  lens outside
  * [0, max_pages page_size] are taken as the nearest of these; results of a sequence whose pages

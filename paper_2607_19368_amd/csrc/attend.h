@@ -88,6 +88,7 @@ struct AttendArgs {
   int splits;             // of a packed sequence's or of a paged sequence's own keys
   int pre_splits;         // of the prefix, slots in front of the others
   int pre_tiles;          // row tiles of the prefix in this launch (0: not in it)
+  int chain;              // the prefix's keys stand in front of each sequence's own (attend_rows.h)
   int64_t rows;           // tokens * Hq
   uint64_t by_heads, by_splits, by_pre_splits;   // at_divisor() of Hkv and the splits
   float* part_o;          // [slot][rows][d] sum p v, NULL: one split, results go to out

@@ -29,7 +29,8 @@ struct AttendPart {
   double us;
 };
 struct AttendPlan {
-  AttendPart own, pre;    // of the packed or the sequences' own keys; of the prefix (tiles 0: none)
+  AttendPart own, pre;    // of the packed or the sequences' own keys; of the prefix (tiles 0: none for itself)
+  bool chain;             // the prefix in front of each sequence's own keys, no part for itself
   int slots;              // partial results of a row (1: none are written)
   int64_t bytes;
 };
@@ -51,36 +52,39 @@ struct AttendCost { int rows; double start, one, pair, full; };
 static const AttendCost ATTEND_COSTS[4] = {
     {16, 1.8, 0.65, 0.8, 0.33}, {32, 2.5, 0.75, 0.95, 0.42}, {AT_ROWS / 2, 2.6, 0.78, 1.1, 0.55}, {AT_ROWS, 3.0, 1.13, 1.75, 0.95}};
 static const double ATTEND_LAUNCH = 4.0;
+static const double ATTEND_SECOND = 2.0;         // of a second launch, where it is the host that is waited for
 // Partial results: another pass over memory, the end of the blocks that write them, and a launch.
 static double attend_join_us(int64_t slots, int64_t rows, int d) {
   return slots > 1 ? 3.0 + 0.1 * (double)slots + 1.35 * (double)(slots * rows) * (4.0 * d + 8.0) / 3.5e6 : 0.0;
 }
 
-// The kernel and the splits that cost least for `sets` runs of `rows` rows a key/value head against `keys` keys
-// each, of which a row tile sees `mean` on average.  out_rows: rows of a partial result.  also: other
-// partial results of a row; same: the kernel of a launch that this one would join.
+// The kernel and the splits (at most max_splits) that cost least for `sets` runs of `rows` rows a key/value head
+// against `keys` keys each, of which a row tile sees `mean` on average and the share `fresh` is no other run's
+// too.  out_rows: rows of a partial result.  also: other partial results of a row; same: the kernel of a launch
+// that this one would join.
 static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys, double mean, int64_t out_rows,
-                              int d, int n_cu,
-                              int also, int same, bool paged) {
+                              int d, int n_cu, int also, int same, bool paged, int max_splits, double fresh) {
   AttendPart best = {};
   best.us = INFINITY;
   best.rows = 16, best.splits = 1;
   // part of a block's time does not shrink with d: 4 heads of 64, 256 rows against 2256 keys, 0.79 us a tile of 128
   // rows, 0.57 of 64, 0.52 of 32
   const double work = 0.4 + 0.6 * d / 128.0, part = keys > 0 ? mean / (double)keys : 1.0;
-  const int64_t units = (keys + 63) / 64, most = std::max<int64_t>(1, std::min<int64_t>(64, units)), slots = 2 * (int64_t)n_cu;
+  const int64_t units = (keys + 63) / 64, most = std::max<int64_t>(1, std::min<int64_t>(max_splits, units));
+  const int64_t slots = 2 * (int64_t)n_cu;
   for (const AttendCost& c : ATTEND_COSTS) {
     if (paged && c.rows == AT_ROWS / 2) continue;
     const int64_t per = std::max<int64_t>(1, (rows + c.rows - 1) / c.rows), tiles = sets * per, base = tiles * Hkv;
-    // a unit's 64 keys come from memory at 5.2 TB/s, once for the row tiles that share them
-    const double mem = 256.0 * d * n_cu / 5.2e6 / (double)per;
-    const double full = std::max(c.full * work, mem), one = std::max(c.one * work, mem),
-                 pair = std::max(c.pair * work, 2.0 * mem);
+    // a unit's 64 keys come from memory at 5.2 TB/s, for the row tiles that share them once, and from the
+    // caches at four times that
+    const double mem = fresh * 256.0 * d * n_cu / 5.2e6 * (0.25 + 0.75 / (double)per);
+    const double full = c.full * work, pair = c.pair * work;
     const int64_t fill = slots / std::max<int64_t>(1, base);
     for (const int64_t want : {(int64_t)1, (int64_t)2, (int64_t)3, fill / 2, fill, 2 * fill, 4 * fill, most}) {
       const int64_t s = std::max<int64_t>(1, std::min(want, most)), n = (units + s - 1) / s, blocks = base * s;
       const int64_t rounds = blocks / slots, rest = blocks - rounds * slots;
       const double each = (double)n * part, two = rounds > 1 || (rounds == 1 && rest) ? 2.0 * full : std::min(pair, 2.0 * full);
+      const double one = std::max(c.one * work, mem * std::min(1.0, 0.4 + (double)blocks / n_cu));     // few draw less
       double us;
       if (part < 1.0) {
         // causal, the blocks with the most keys first, down to 2 part - 1 of the longest: the longest has one
@@ -96,6 +100,7 @@ static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys,
       } else {
         us = (double)rounds * (each * two + 2.0 * c.start) + (rest == 0 ? 0.0 : each * (rest <= n_cu ? one : two) + c.start);
       }
+      us = std::max(us, (double)blocks / n_cu * each * mem + c.start);
       us += (same && (c.rows == same || c.rows == AT_ROWS) ? 0.0 : ATTEND_LAUNCH) + attend_join_us(s + also, out_rows, d);
       if (blocks + sets * Hkv * s > AT_BLOCKS / 2 - 64) us += 1e12;      // a launch may be of two plans
       if (us < best.us) best = AttendPart{c.rows, (int)s, tiles, us};
@@ -114,7 +119,7 @@ static AttendPlan attend_plan_packed(int64_t Tq, int64_t Tk, int B, int Hq, int 
   // as if the sequences were equal; where they are not, their tiles are B more at most
   const int64_t rows = Tq * (Hq / Hkv), n = std::max(1, B), keys = Tk / n;
   const double mean = causal ? std::max((double)keys / 2, (double)keys - (double)Tq / n / 2) : (double)keys;
-  p.own = attend_part((rows + n - 1) / n, n, Hkv, keys, mean, Tq * Hq, d, attend_cus(), 0, 0, false);
+  p.own = attend_part((rows + n - 1) / n, n, Hkv, keys, mean, Tq * Hq, d, attend_cus(), 0, 0, false, 64, 1.0);
   p.own.tiles = rows / p.own.rows + B;
   attend_finish(p, Tq * Hq, d);
   return p;
@@ -124,9 +129,27 @@ static AttendPlan attend_plan_paged(int B, int n_q, int Hq, int Hkv, int d, int6
   AttendPlan p = {};
   const int n_cu = attend_cus();
   const int64_t rows = (int64_t)n_q * (Hq / Hkv), out_rows = (int64_t)B * n_q * Hq;
-  p.own = attend_part(rows, B, Hkv, max_len, (double)max_len, out_rows, d, n_cu, prefix_len > 0, 0, true);
-  if (prefix_len > 0)
-    p.pre = attend_part(B * rows, 1, Hkv, prefix_len, (double)prefix_len, out_rows, d, n_cu, p.own.splits, p.own.rows, true);
+  p.own = attend_part(rows, B, Hkv, max_len, (double)max_len, out_rows, d, n_cu, prefix_len > 0, 0, true, 64, 1.0);
+  if (prefix_len > 0) {
+    p.pre = attend_part(B * rows, 1, Hkv, prefix_len, (double)prefix_len, out_rows, d, n_cu, p.own.splits, p.own.rows, true, 64, 1.0);
+    // A short prefix is read by each sequence in front of its own keys: one launch instead of two and no
+    // partial results.  28 / 4 heads of 128, prefix + own keys, us in a graph / of a call, as parts and so:
+    //   8 sequences, 512 + 100        9.0 / 15.4    10.4 / 12.4 (10.3 where calls follow each other)
+    //   64, 512 + 64                 14.8 / 15.2    10.2 / 12.0
+    //   8, 1000 + 100                10.1 / 15.4    15.2 / 15.0: parts
+    //   1, 1400 + 100                 8.5 / 15.4    18.6 / 18.2: parts
+    // (32 sequences of 5 tokens, 32 / 8 heads, 300 + 60: 18.1 in parts, 10.8 so)
+    const AttendPart c = attend_part(rows, B, Hkv, prefix_len + max_len, (double)(prefix_len + max_len), out_rows, d, n_cu,
+                                     0, 0, true, 1, ((double)prefix_len / B + max_len) / (double)(prefix_len + max_len));
+    const bool beside = (p.own.tiles * p.own.splits + p.pre.tiles * p.pre.splits) * Hkv <= n_cu;
+    const double parts = beside ? std::max(p.own.us, p.pre.us + ATTEND_LAUNCH)
+                                : p.own.us + p.pre.us - attend_join_us(p.own.splits + 1, out_rows, d);
+    if (c.rows != AT_ROWS && c.us < parts + ATTEND_SECOND) {
+      p.chain = true;
+      p.own = c;
+      p.pre = AttendPart{};
+    }
+  }
   attend_finish(p, out_rows, d);
   return p;
 }
@@ -152,6 +175,7 @@ static int attend_run(AttendArgs& a, const AttendPlan& p, bool paged, bool bf16,
   };
   (void)hipGetLastError();
   a.pre_tiles = (int)p.pre.tiles;
+  a.chain = p.chain;
   hipError_t e;
   if (pre && p.pre.rows == AT_ROWS && p.own.rows != AT_ROWS) {
     e = launch_attend_both(a, bf16, p.own.rows, d, pre, pre + own, s);

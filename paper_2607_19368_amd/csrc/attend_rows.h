@@ -8,11 +8,13 @@
 // is no barrier, only each wave's wait for its own loads, which go straight to LDS a step ahead.
 // 16 keys a step: a wave's two stages of K and V are 16 KB (d = 128), so that two blocks fit a
 // compute unit and one's start and end hide behind the other's steps; and pages of 16 rows or
-// more hold whole steps, which makes their addresses uniform.
+// more hold whole steps, which makes their addresses uniform.  A short prefix (chain) is steps in front of
+// a sequence's own.
 //
 // Measured, d = 128: two new tokens of 6 sequences of up to 49159 fp16 rows in pages of 32, 32 / 8 heads:
-// 987 MB in 174 us = 5.7 TB/s (179 with the join; a pure read of large buffers reaches 6.55 TB/s, a copy 4.75).  512 causal
-// bf16 tokens, 28 / 4 heads: 12.6 us, the dependent chain of 8 steps of 0.6 us behind the launch.
+// 987 MB in 175 us = 5.6 TB/s (180 with the join; a pure read of large buffers reaches 6.55 TB/s, a copy 4.75).  512 causal
+// bf16 tokens, 28 / 4 heads: 12.7 us, the dependent chain of 8 steps of 0.6 us behind the launch.  8 sequences of 97
+// rows behind 512, 28 / 4 heads: 10.3 us, 10 such steps.
 #pragma once
 #include "attend.h"
 
@@ -66,8 +68,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
 
   const int end = max(0, at_sees(t, (t.r1 - 1) / a.g));
   const int least = __builtin_amdgcn_readfirstlane(at_sees(t, t.r0 / a.g));
-  // steps of this split, in fours for the waves
-  const int all = (end + RW_KEYS - 1) / RW_KEYS;
+  // steps of this split, in fours for the waves; steps [0, up) are those of a prefix in front
+  const int up = PAGED && a.chain ? (a.prefix_len + RW_KEYS - 1) / RW_KEYS : 0;
+  const int all = up + (end + RW_KEYS - 1) / RW_KEYS;
   const int each = ((all + t.n_split - 1) / t.n_split + AT_WAVES - 1) / AT_WAVES * AT_WAVES;
   const int u0 = min((int64_t)all, (int64_t)t.split * each), u1 = min(all, u0 + each);
 
@@ -93,10 +96,10 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
   // (pages are not written while the kernel runs, hence the constant address space).
   auto page_of = [&](int u) {
     if (!PAGED || !even_pages) return 0;
-    return ((at_const_ints)t.list)[(u * RW_KEYS) >> a.lg_page];
+    return ((at_const_ints)(u < up ? a.prefix_pages : t.list))[((u < up ? u : u - up) * RW_KEYS) >> a.lg_page];
   };
   auto load = [&](int u, int page, uint16_t* to) {
-    const int j0 = u * RW_KEYS;
+    const int j0 = (u < up ? u : u - up) * RW_KEYS;
     if (PAGED ? even_pages : j0 + RW_KEYS <= t.nk) {
       const uint16_t *kt = kbase, *vt = vbase;
       if (PAGED) {
@@ -115,9 +118,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
     }
 #pragma unroll
     for (int x = 0; x < NL; ++x) {
-      int64_t r = min(j0 + row_of(x), t.nk - 1);
+      int64_t r = min(j0 + row_of(x), (u < up ? a.prefix_len : t.nk) - 1);
       if (PAGED) {                                 // pages of fewer than 16 rows: one a row
-        const int p = t.list[r >> a.lg_page];
+        const int p = (u < up ? a.prefix_pages : t.list)[r >> a.lg_page];
         r = (((int64_t)((unsigned)p < (unsigned)a.n_pages ? p : 0) * a.Hkv + kvh) << a.lg_page) + (r & in_page);
       }
       __builtin_amdgcn_global_load_lds((at_gptr)(kbase + r * k_st + k_chunk(x)), (at_lptr)(to + x * 512), 16, 0, 0);
@@ -172,8 +175,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
     else
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
-    const int j0 = u * RW_KEYS;
-    const bool masked = least < j0 + RW_KEYS;
+    const bool pre = u < up;                       // every row sees the whole prefix
+    const int j0 = (pre ? u : u - up) * RW_KEYS;
+    const bool masked = (pre ? a.prefix_len : least) < j0 + RW_KEYS;
     if (masked) {
       // 0 x inf in the product would reach rows that do not see the key: infinite and NaN values
       // (rare) are added to the rows that see them, and leave the step before the products
@@ -197,7 +201,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
               if ((v & (TY::EXP & 0xffff)) == (TY::EXP & 0xffff)) {
 #pragma unroll
                 for (int n = 0; n < NR; ++n)
-                  if (j0 + r < limit[n]) o[n][b][e] += TY::value(v);
+                  if (j0 + r < (pre ? a.prefix_len : limit[n])) o[n][b][e] += TY::value(v);
               }
             }
 #pragma unroll
@@ -229,7 +233,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       if (masked) {
-        int left = limit[n] - j0 - 4 * grp;
+        int left = (pre ? a.prefix_len : limit[n]) - j0 - 4 * grp;
         asm volatile("" : "+v"(left));             // a branch, not selects in every step
 #pragma unroll
         for (int e = 0; e < 4; ++e)

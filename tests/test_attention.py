@@ -558,6 +558,25 @@ def test_paged_many_splits_of_few_rows(d, dt):
     _paged_case(2, 1, 4, 2, d, dt, 16, 0, [4100, 1], d + 1)
 
 
+@gpu
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+def test_paged_prefixes_read_by_each_sequence_and_by_all(d, dt):
+    """A short prefix stands in front of every sequence's own keys, a long one has blocks of its own: ends inside
+    a step and a page, sequences without own keys, several new tokens."""
+    _paged_case(24, 1, 8, 2, d, dt, 16, 131, [b % 9 + (b > 2) * 11 for b in range(24)], d)
+    _paged_case(3, 5, 6, 3, d, dt, 4, 77, [64, 3, 0], d + 1)
+    _paged_case(2, 3, 14, 2, d, dt, 32, 1501, [3, 20], d + 2)
+    _paged_case(40, 3, 8, 1, d, dt, 64, 3001, [3 + b for b in range(40)], d + 3)
+
+
+@gpu
+@pytest.mark.parametrize("d,dt", [(64, HF), (128, BF)])
+def test_paged_many_rows_against_a_long_prefix(d, dt):
+    """The prefix in tiles of many rows, the own keys by few."""
+    _paged_case(128, 2, 28, 1, d, dt, 32, 3001, [2 + (5 * b) % 31 for b in range(128)], d)
+
+
 # ---------------------------------------------------------------- refusals
 def test_library_refuses_before_any_gpu_work():
     lib = B.load()
