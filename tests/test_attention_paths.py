@@ -137,7 +137,7 @@ class Packed:
 
     def __init__(self, shape, d, dt, causal):
         self.Tq, self.Tk, self.n, self.Hq, self.Hkv = shape
-        self.d, self.causal = d, causal
+        self.d, self.causal, self.scale = d, causal, None
         g = torch.Generator(device="cuda")
         g.manual_seed(d + self.Tq)
         self.lq, self.lk = lengths(self.Tq, self.Tk, self.n, d)
@@ -150,8 +150,8 @@ class Packed:
         """Output and lse; every row belongs to a sequence."""
         out = torch.full((self.Tq, self.Hq, self.d), 7.0, dtype=self.q.dtype, device="cuda")
         lse = torch.full((self.Tq, self.Hq), 7.0, device="cuda")
-        P.slh_attend(self.q, self.k if k is None else k, self.v if v is None else v, self.cq, self.ck, causal=self.causal,
-                     out=out, lse_out=lse)
+        P.slh_attend(self.q, self.k if k is None else k, self.v if v is None else v, self.cq, self.ck, scale=self.scale,
+                     causal=self.causal, out=out, lse_out=lse)
         return out, lse
 
     def sequences(self):
@@ -212,7 +212,7 @@ class Paged:
 
     def __init__(self, shape, d, dt):
         self.n, self.n_q, self.Hq, self.Hkv, page, width, self.prefix = shape
-        self.d, self.page = d, page
+        self.d, self.page, self.scale = d, page, None
         g = torch.Generator(device="cuda")
         g.manual_seed(d + self.prefix)
         r = random.Random(d)
@@ -244,7 +244,8 @@ class Paged:
     def run(self):
         lse = torch.full(self.q.shape[:3], 7.0, device="cuda")
         out = torch.full_like(self.q, 7.0)
-        P.slh_attend_paged(self.q, self.kc, self.vc, self.table, self.len_, self.pre, self.prefix, out=out, lse_out=lse)
+        P.slh_attend_paged(self.q, self.kc, self.vc, self.table, self.len_, self.pre, self.prefix, scale=self.scale, out=out,
+                           lse_out=lse)
         return out, lse
 
     def keys(self, b):
@@ -284,3 +285,97 @@ def test_paged_paths_unseen_values(shape, d, dt, bad):
     want = clean.clone()
     want[0, -1, (c.Hkv - 1) * c.Hq // c.Hkv:, 5] = bad
     assert torch.equal(c.run()[0].nan_to_num(nan=9.0), want.nan_to_num(nan=9.0))
+
+
+# ---------------------------------------------------------------- partial results: graphs, streams, dirty memory
+def _splits(pre, own):
+    """Packed (lengths of keys) and paged (lengths) calls whose keys are split, more and less full."""
+    return [(pre, own), (0, 1), (pre // 3, own // 2), (pre, 0), (5, own)]
+
+
+@gpu
+@pytest.mark.parametrize("lq,heads,d", [(20, (4, 2), 64), (130, (16, 1), 128)])          # joined by four waves, by one
+def test_packed_splits_in_a_graph_and_on_another_stream(lq, heads, d):
+    """Partial results in memory that holds NaN before each replay, with splits that are empty in some: the eager
+    call's bits."""
+    Hq, Hkv = heads
+    most = 6000
+    need = P.slh_attend_workspace(lq, most, 2, Hq, Hkv, d)
+    assert need > 0
+    g = torch.Generator(device="cuda")
+    g.manual_seed(lq)
+    q = torch.randn(lq, Hq, d, generator=g, device="cuda").to(BF)
+    k, v = (torch.randn(most, Hkv, d, generator=g, device="cuda").to(BF) for _ in range(2))
+    cq = torch.tensor([0, lq // 2, lq], dtype=torch.int32, device="cuda")
+    ck = torch.tensor([0, 2500, most], dtype=torch.int32, device="cuda")
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(lq, Hq, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.slh_attend(q, k, v, cq, ck, out=out, lse_out=lse, workspace=ws)
+    side = torch.cuda.Stream()
+    for a, b in _splits(2500, 3500):
+        ck.copy_(torch.tensor([0, a, a + b], dtype=torch.int32))
+        q.copy_(torch.randn(lq, Hq, d, generator=g, device="cuda"))
+        want_lse = torch.empty_like(lse)
+        want = P.slh_attend(q, k, v, cq, ck, lse_out=want_lse)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        for rows, keys in ((slice(0, lq // 2), slice(0, a)), (slice(lq // 2, lq), slice(a, a + b))):
+            n, m = rows.stop - rows.start, keys.stop - keys.start
+            o, tol, e, etol = rows_of(q[rows], k[keys], v[keys], [m - n + i + 1 for i in range(n)], d ** -0.5)
+            close(out[rows], o, tol, f"{a} and {b} keys")
+            close_lse(lse[rows], e, etol, f"{a} and {b} keys")
+        ws.fill_(255)
+        out.fill_(7.0)
+        side.wait_stream(torch.cuda.current_stream())
+        P.slh_attend(q, k, v, cq, ck, out=out, workspace=ws, stream=side)
+        side.synchronize()
+        assert torch.equal(out, want)
+
+
+@gpu
+@pytest.mark.parametrize("n,heads,prefix", [(2, (8, 2), 3000), (40, (28, 4), 3000), (128, (28, 1), 9000)])
+def test_paged_splits_in_a_graph_and_on_another_stream(n, heads, prefix):
+    """As above behind a prefix, whose parts are rows or tiles, with own lengths that change."""
+    (Hq, Hkv), d, page, width = heads, 128, 16, 40
+    need = P.slh_attend_paged_workspace(n, 1, Hq, Hkv, d, width * page, prefix)
+    assert need > 0
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    n_pre = -(-prefix // page)
+    kc, vc = (torch.randn(n_pre + n * width, Hkv, page, d, generator=g, device="cuda").to(BF) for _ in range(2))
+    pre = torch.arange(n_pre, dtype=torch.int32, device="cuda")
+    table = (n_pre + torch.arange(n * width, dtype=torch.int32, device="cuda")).view(n, width)
+    lens = torch.full((n,), width * page, dtype=torch.int32, device="cuda")
+    q = torch.randn(n, 1, Hq, d, generator=g, device="cuda").to(BF)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(n, 1, Hq, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.slh_attend_paged(q, kc, vc, table, lens, pre, prefix, out=out, lse_out=lse, workspace=ws)
+    side = torch.cuda.Stream()
+    for a, b in _splits(width * page, width * page - 3):
+        lens.copy_(torch.tensor([a if i % 2 else b for i in range(n)], dtype=torch.int32))
+        q.copy_(torch.randn(n, 1, Hq, d, generator=g, device="cuda"))
+        want_lse = torch.empty_like(lse)
+        want = P.slh_attend_paged(q, kc, vc, table, lens, pre, prefix, lse_out=want_lse)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        for i in (0, 1):
+            own = a if i % 2 else b
+            at = (n_pre + i * width) * page
+            kk, vv = (torch.cat([t[:prefix], t[at:at + own]]) for t in (x.permute(0, 2, 1, 3).reshape(-1, Hkv, d) for x in (kc, vc)))
+            o, tol, e, etol = rows_of(q[i], kk, vv, [prefix + own], d ** -0.5)
+            close(out[i], o, tol, f"{own} own keys")
+            close_lse(lse[i], e, etol, f"{own} own keys")
+        ws.fill_(255)
+        out.fill_(7.0)
+        side.wait_stream(torch.cuda.current_stream())
+        P.slh_attend_paged(q, kc, vc, table, lens, pre, prefix, out=out, workspace=ws, stream=side)
+        side.synchronize()
+        assert torch.equal(out, want)
