@@ -529,7 +529,8 @@ int slh_kv_append(const void *k, int64_t k_st, int64_t k_sh, const void *v, int6
  *   out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i . k_j),  j < limit_i
  * limit_i = the sequence's keys, or, where `causal`, keys - queries + i + 1: the last query sees
  * every key, so keys of a cached context may stand before the queries' own.  A query that sees
- * no key gets zeros.  What a query does not see does not reach it, infinities and NaN included.
+ * no key gets zeros; one whose keys all have the score -infinity gets NaN (0 / 0).  What a query does not see does
+ * not reach it, infinities and NaN included.
  * Query head h reads key/value head h / (Hq / Hkv).  dtype: SLH_BF16 or SLH_F16; d: 64, 80, 96 or
  * 128.  Products of dtype with fp32 accumulation, softmax in fp32; the weights are rounded to dtype
  * for the second product.  lse: [Tq][Hq] floats, ln sum_j p_ij (-inf where nothing is seen), or NULL.

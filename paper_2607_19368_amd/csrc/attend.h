@@ -92,7 +92,7 @@ struct AttendArgs {
   int64_t rows;           // tokens * Hq
   uint64_t by_heads, by_splits, by_pre_splits;   // at_divisor() of Hkv and the splits
   float* part_o;          // [slot][rows][d] sum p v, NULL: one split, results go to out
-  float* part_ml;         // [slot][rows][2] maximum (of the unscaled scores) and sum p
+  float* part_ml;         // [slot][rows][2] maximum (of the unscaled scores) and sum p, AT_NO_KEY: the row sees none of its keys
 };
 
 // Transposing LDS read of 16 lanes: 4 rows of 16 elements, lane i gets column i.  `restrict` says
@@ -121,6 +121,13 @@ __device__ __forceinline__ void at_products_done(T (&x)[N]) {
 // accumulated sums are rescaled only when some row of the wave passes it.  Weights up to 2^8
 // lose nothing: their rounding is relative, and fp16 holds up to 2^15.
 constexpr float AT_LAG = 8.f;
+
+// A row that sees no key has the result 0 and no sums, which its limit says and not the sums: keys that it sees may all
+// have the score -inf, and their 0 / 0 is to show.
+constexpr float AT_NO_KEY = -1.f;
+__device__ __forceinline__ float at_inverse(bool no_key, float l) {
+  return no_key ? 0.f : l == 0.f ? __builtin_nanf("") : 1.0f / l;
+}
 
 // A tile's rows are reached by 32-bit offsets in bytes from its first.
 constexpr int64_t AT_STRIDE = (int64_t)1 << 24;

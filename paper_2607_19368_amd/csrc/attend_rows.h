@@ -324,16 +324,17 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
     }
     const int i = row / a.g, h = kvh * a.g + row - i * a.g;
     const int64_t out_row = (t.tok0 + i) * a.Hq + h;
-    const bool empty = top == -INFINITY && sum == 0.f;
+    // sees none of this split's keys
+    const bool empty = u0 >= u1 || (u0 >= up && at_sees(t, i) <= (u0 - up) * RW_KEYS);
     if (a.part_o) {
       const int64_t at = t.slot * a.rows + out_row;
-      if (c == 0) a.part_ml[2 * at] = top, a.part_ml[2 * at + 1] = sum;
+      if (c == 0) a.part_ml[2 * at] = top, a.part_ml[2 * at + 1] = empty ? AT_NO_KEY : sum;
       if (empty) continue;                         // its sums are not read
       *(at_f32x4*)(a.part_o + at * D + 8 * c) = v0;
       *(at_f32x4*)(a.part_o + at * D + 8 * c + 4) = v1;
       continue;
     }
-    const float inv = empty ? 0.f : 1.0f / sum;
+    const float inv = at_inverse(empty, sum);
     at_u32x4 w;
     w[0] = TY::pack(v0[0] * inv, v0[1] * inv);
     w[1] = TY::pack(v0[2] * inv, v0[3] * inv);

@@ -400,14 +400,14 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
         for (int f = 0; f < 4; ++f) o[b][e + f] = __builtin_fmaf(k1, o[b][e + f], k2 * x[f]);
       }
   }
-  const bool empty = m == -INFINITY && l == 0.f;
+  const bool empty = t0 >= t1 || limit <= t0 * AT_KEYS;      // sees none of this split's keys
   const int64_t r = (t.tok0 + i) * a.Hq + h;
   if (a.part_o) {
     if (!real) return;
     const int64_t at = t.slot * a.rows + r;
     if (half == 0) {
       a.part_ml[2 * at] = m;
-      a.part_ml[2 * at + 1] = l;
+      a.part_ml[2 * at + 1] = empty ? AT_NO_KEY : l;
     }
     if (empty) return;                             // its sums are not read
     float* op = a.part_o + at * D;
@@ -421,7 +421,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
       }
     return;
   }
-  const float inv = empty ? 0.f : 1.0f / l;
+  const float inv = at_inverse(empty, l);
   uint16_t* op = a.out + (t.tok0 + i) * a.o_st + h * a.o_sh + 8 * half;
 #pragma unroll
   for (int b = 0; b < DB; ++b)

@@ -55,8 +55,8 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
   // packed rows in front of the first sequence or behind the last have no results
   if (a.cu_q && (tok < a.cu_q[0] || tok >= a.cu_q[a.B])) return;
   auto ml = [&](int s) { return *(const float2*)(a.part_ml + 2 * (s * a.rows + r)); };
-  auto is_empty = [](float2 v) { return v.x == -INFINITY && v.y == 0.f; };
-  const float2 none = make_float2(-INFINITY, 0.f);
+  auto is_empty = [](float2 v) { return v.y == AT_NO_KEY; };
+  const float2 none = make_float2(-INFINITY, AT_NO_KEY);
   const float2 first = lane < slots ? ml(lane) : none;
   float top = first.x;
   bool any = !is_empty(first);
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
       for (int c = 0; c < 4; ++c) o[c] += x[c];
     }
   }
-  const float inv = empty ? 0.f : 1.0f / l;
+  const float inv = at_inverse(empty, l);
   if (half == 0 && e < d)
     *(at_u32x2*)(a.out + tok * a.o_st + h * a.o_sh + e) =
         at_u32x2{TY::pack(o[0] * inv, o[1] * inv), TY::pack(o[2] * inv, o[3] * inv)};

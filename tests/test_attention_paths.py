@@ -379,3 +379,61 @@ def test_paged_splits_in_a_graph_and_on_another_stream(n, heads, prefix):
         P.slh_attend_paged(q, kc, vc, table, lens, pre, prefix, out=out, workspace=ws, stream=side)
         side.synchronize()
         assert torch.equal(out, want)
+
+
+# ---------------------------------------------------------------- keys that are seen and weigh nothing
+def _broken_key(k, head):
+    """The element of every key of a head that makes its score with a query of ones there -inf."""
+    k = k.clone()
+    k[:, head, 3] = -math.inf
+    return k
+
+
+@gpu
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("shape", PACKED)
+def test_packed_rows_whose_keys_all_score_minus_infinity(shape, dt):
+    """0 / 0 by the definition, so NaN, with lse -inf: not the zeros of a row that sees no key, which stay.  With one
+    finite score among them such keys weigh nothing."""
+    c = Packed(shape, 64, dt, True)
+    c.q[:, :, 3] = 1.0
+    head = c.Hkv - 1
+    heads = slice(head * c.Hq // c.Hkv, c.Hq)
+    want, want_lse = c.run()
+    k = _broken_key(c.k, head)
+    got, lse = c.run(k=k)
+    for rq, rk, limit in c.sequences():
+        blind = sum(x <= 0 for x in limit)
+        assert not bool(got[rq.start:rq.start + blind].any())
+        assert bool(torch.isnan(got[rq.start + blind:rq.stop, heads]).all())
+        assert bool((lse[rq, heads] == -math.inf).all())
+        got[rq, heads], lse[rq, heads] = want[rq, heads], want_lse[rq, heads]
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    rq, rk, limit = max(c.sequences(), key=lambda s: min(s[0].stop - s[0].start, s[1].stop - s[1].start))
+    k[rk.start, head] = c.k[rk.start, head]                       # the one key of finite score
+    got, lse = c.run(k=k)
+    blind = sum(x <= 0 for x in limit)
+    assert not bool(got[rq.start:rq.start + blind, heads].any())
+    assert torch.equal(got[rq.start + blind:rq.stop, heads], c.v[rk.start, head].expand(len(limit) - blind, heads.stop - heads.start, 64))
+    s = c.q[rq, heads].double() @ c.k[rk.start, head].double() / 8
+    e = 2 * (64 + 8) * 2.0 ** -24 * (c.q[rq, heads].double().abs() @ c.k[rk.start, head].double().abs() / 8 + 1) + 9 * 2.0 ** -24 * (1 + s.abs())
+    assert bool(((lse[rq, heads].double() - s).abs() <= e)[blind:].all())
+
+
+@gpu
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("shape", PAGED)
+def test_paged_rows_whose_keys_all_score_minus_infinity(shape, dt):
+    c = Paged(shape, 64, dt)
+    c.q[..., 3] = 1.0
+    head = c.Hkv - 1
+    heads = slice(head * c.Hq // c.Hkv, c.Hq)
+    want, want_lse = c.run()
+    c.kc[:, head, :, 3] = -math.inf
+    got, lse = c.run()
+    limit = torch.tensor([[c.prefix + max(0, x - c.n_q + i + 1) for i in range(c.n_q)] for x in c.lens], device="cuda")
+    broken = got[:, :, heads]
+    assert bool(torch.isnan(broken[limit > 0]).all()) and not bool(broken[limit == 0].any())
+    assert bool((lse[:, :, heads] == -math.inf).all())
+    got[:, :, heads], lse[:, :, heads] = want[:, :, heads], want_lse[:, :, heads]
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
