@@ -25,6 +25,7 @@ struct AtBf16 {
   typedef at_bf16x8 vec;
   static constexpr uint32_t EXP = 0x7f807f80u;       // exponent bits of two elements
   static constexpr uint32_t CARRY = 0x00800080u;     // carries into the sign bit from a full exponent
+  static constexpr float LIFT = 0.f;                 // the range is fp32's
   __device__ static at_f32x16 mfma(at_u32x4 a, at_u32x4 b, at_f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(vec, a), __builtin_bit_cast(vec, b), c, 0, 0, 0);
   }
@@ -44,6 +45,7 @@ struct AtF16 {
   typedef at_f16x8 vec;
   static constexpr uint32_t EXP = 0x7c007c00u;
   static constexpr uint32_t CARRY = 0x04000400u;
+  static constexpr float LIFT = 7.f;                 // up to 2^15 with AT_LAG; full precision down to 2^-21 of the maximum
   __device__ static at_f32x16 mfma(at_u32x4 a, at_u32x4 b, at_f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(vec, a), __builtin_bit_cast(vec, b), c, 0, 0, 0);
   }
@@ -118,8 +120,9 @@ __device__ __forceinline__ void at_products_done(T (&x)[N]) {
 }
 
 // A row's weights are taken relative to a maximum that may lag behind by up to 2^AT_LAG: the
-// accumulated sums are rescaled only when some row of the wave passes it.  Weights up to 2^8
-// lose nothing: their rounding is relative, and fp16 holds up to 2^15.
+// accumulated sums are rescaled only when some row of the wave passes it.  All weights (and so their sums, which
+// the results are divided by) are raised by 2^LIFT of the type: those that are rounded to fp16, whose smallest step
+// is 2^-24, would otherwise be lost below 2^-25 of the maximum, however many there are.
 constexpr float AT_LAG = 8.f;
 
 // A row that sees no key has the result 0 and no sums, which its limit says and not the sums: keys that it sees may all

@@ -255,12 +255,12 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
           for (int e = 0; e < 4; ++e) o[n][b][e] *= keep;
       }
       const float at = m[n] == -INFINITY ? 0.f : m[n];       // a row that has seen no key yet
-      float mu = at * a.c;
+      float mu = __builtin_fmaf(at, a.c, -TY::LIFT);
       if (a.c > 1.f) {
         // the largest scores times c are past fp32: the maximum leaves them first
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[n][e] -= at;
-        mu = 0.f;
+        mu = -TY::LIFT;
       }
       float p[4];
 #pragma unroll
@@ -342,7 +342,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, int block, uint
     w[3] = TY::pack(v1[2] * inv, v1[3] * inv);
     *(at_u32x4*)(a.out + (t.tok0 + i) * a.o_st + h * a.o_sh + 8 * c) = w;
     if (a.lse && c == 0)
-      a.lse[out_row] = empty ? -INFINITY : top * a.scale + 0.69314718f * __builtin_amdgcn_logf(sum);
+      a.lse[out_row] = empty ? -INFINITY : top * a.scale + 0.69314718f * (__builtin_amdgcn_logf(sum) - TY::LIFT);
   }
 }
 

@@ -262,14 +262,14 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
         for (int e = 0; e < 16; ++e) o[b][e] *= keep;
     }
     const float at = m == -INFINITY ? 0.f : m;     // a row that has seen no key yet
-    float mu = at * a.c;
+    float mu = __builtin_fmaf(at, a.c, -TY::LIFT);
     if (a.c > 1.f) {
       // the largest scores times c are past fp32: the maximum leaves them first
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[kb][e] -= at;
-      mu = 0.f;
+      mu = -TY::LIFT;
     }
     float sum0 = 0.f, sum1 = 0.f;
     at_u32x4 pf[2 * NB];                                // P^T, 16 keys each
@@ -436,7 +436,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
       if (real && d < D) *(at_u32x4*)(op + d) = at_u32x4{w0[0], w1[0], w0[1], w1[1]};
     }
   if (a.lse && real && half == 0)
-    a.lse[r] = empty ? -INFINITY : m * a.scale + 0.69314718f * __builtin_amdgcn_logf(l);
+    a.lse[r] = empty ? -INFINITY : m * a.scale + 0.69314718f * (__builtin_amdgcn_logf(l) - TY::LIFT);
 }
 
 }  // namespace slh

@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
   if (half == 0 && e < d)
     *(at_u32x2*)(a.out + tok * a.o_st + h * a.o_sh + e) =
         at_u32x2{TY::pack(o[0] * inv, o[1] * inv), TY::pack(o[2] * inv, o[3] * inv)};
-  if (a.lse && lane == 0) a.lse[r] = empty ? -INFINITY : top * a.scale + 0.69314718f * __builtin_amdgcn_logf(l);
+  if (a.lse && lane == 0) a.lse[r] = empty ? -INFINITY : top * a.scale + 0.69314718f * (__builtin_amdgcn_logf(l) - TY::LIFT);
 }
 
 hipError_t launch_attend_join(const AttendArgs& a, bool bf16, int d, int slots, hipStream_t s) {

@@ -437,3 +437,78 @@ def test_paged_rows_whose_keys_all_score_minus_infinity(shape, dt):
     assert bool((lse[:, :, heads] == -math.inf).all())
     got[:, :, heads], lse[:, :, heads] = want[:, :, heads], want_lse[:, :, heads]
     assert torch.equal(got, want) and torch.equal(lse, want_lse)
+
+
+# ---------------------------------------------------------------- light weights
+LIGHT = 17.5                                      # exp(-17.5) = 2^-25.2
+
+
+def light(d, keys):
+    """Output of a row that sees `keys` of keys whose every 16th, the first among them, has the score 0 and the value
+    0, the others the score -LIGHT and the value 1024; and its tolerance.
+
+    A light weight is less than half the smallest step of fp16, 2^-24: it has to be raised before it is rounded.
+    Raised by 2^7 its rounding is 2^-32 of a heavy one at most.  Besides, u of the output for its own rounding and u for
+    the weights' where they are normal, half the smallest step of the output, and 2 (e + keys 2^-24) of the
+    output for fp32 sums and scores that are off by e = 2 (d + 8) 2^-24 (LIGHT + 1)."""
+    heavy = -(-keys // 16)
+    w = (keys - heavy) * math.exp(-LIGHT)
+    o = 1024 * w / (heavy + w)
+    e = 2 * (d + 8) * 2.0 ** -24 * (LIGHT + 1)
+    return o, 1.02 * (2 * 2.0 ** -11 * o + 1024 * 2.0 ** -32 * (keys - heavy) / heavy) + 2 * (e + keys * 2.0 ** -24) * o + 2.0 ** -25
+
+
+def light_rows(n, d):
+    """n keys and values as above."""
+    k, v = torch.zeros(n, d, dtype=HF, device="cuda"), torch.full((n, d), 1024.0, dtype=HF, device="cuda")
+    k[:, 0] = -LIGHT
+    k[::16], v[::16] = 0.0, 0.0
+    return k, v
+
+
+def close_light(got, limit, d, what):
+    for i, n in enumerate(limit):
+        o, tol = light(d, n) if n > 0 else (0.0, 0.0)
+        over = float((got[i].double() - o).abs().max())
+        assert over <= tol, f"{what}, row {i} of {n} keys: {over:.3g} > {tol:.3g} of {o:.3g}"
+
+
+@gpu
+@pytest.mark.parametrize("d", SIZES)
+@pytest.mark.parametrize("shape", PACKED)
+def test_packed_light_weights_count_in_fp16(shape, d):
+    c = Packed(shape, d, HF, True)
+    c.scale = 1.0
+    c.q.zero_()
+    c.q[..., 0] = 1.0
+    for _, rk, _ in c.sequences():
+        c.k[rk], c.v[rk] = (x[:, None] for x in light_rows(rk.stop - rk.start, d))
+    got, lse = c.run()
+    for b, (rq, rk, limit) in enumerate(c.sequences()):
+        some = list(range(0, len(limit), max(1, len(limit) // 40))) + [len(limit) - 1] * (len(limit) > 0)
+        close_light(got[rq][some], [limit[i] for i in some], d, f"sequence {b}")
+        for i in some:
+            if limit[i] > 0:
+                heavy = -(-limit[i] // 16)
+                want = math.log(heavy + (limit[i] - heavy) * math.exp(-LIGHT))
+                assert float((lse[rq][i].double() - want).abs().max()) <= 2 * (d + 8) * 2.0 ** -24 * (LIGHT + 1) + (limit[i] + 8) * 2.0 ** -24 * (1 + want)
+
+
+@gpu
+@pytest.mark.parametrize("d", SIZES)
+@pytest.mark.parametrize("shape", PAGED)
+def test_paged_light_weights_count_in_fp16(shape, d):
+    c = Paged(shape, d, HF)
+    c.scale = 1.0
+    c.q.zero_()
+    c.q[..., 0] = 1.0
+    c.lens[:] = [x // 16 * 16 for x in c.lens]    # ratios as of whole sixteens, behind a prefix of whole sixteens
+    c.prefix = c.prefix // 16 * 16
+    c.len_.copy_(torch.tensor(c.lens))
+    for pages, n in [(c.pre, c.prefix)] + [(c.table[b], c.lens[b]) for b in range(c.n)]:
+        k, v = light_rows(n, d)
+        at = torch.arange(n, device="cuda")
+        c.kc[pages[at // c.page].long(), :, at % c.page], c.vc[pages[at // c.page].long(), :, at % c.page] = k[:, None], v[:, None]
+    got, _ = c.run()
+    for b in range(min(c.n, 5)):
+        close_light(got[b], [c.prefix + max(0, c.lens[b] - c.n_q + i + 1) for i in range(c.n_q)], d, f"sequence {b}")
