@@ -107,14 +107,17 @@ __device__ __forceinline__ at_u32x2 at_tr_read(const uint16_t* __restrict__ p) {
 // The wait states between a matrix product and the first read of its result, which the compiler counts and
 // fills.  Where two ways lead from the one to the other, of which the first that it follows is the longer and
 // still shorter than the wait, it does not count the other (a short branch between them: scores that were read
-// too early, here).  So they are spent in front of such branches: 11 states of a 16 x 16 x 32 product, and as
-// many of a 32 x 32 x 16.  The empty statements keep every product of x in front of the wait and every read
-// of its results behind.
+// too early, here).  So they are spent in front of such branches: 8 states behind a 16 x 16 product, 12 behind a
+// 32 x 32 x 16 one, as many as the compiler fills where nothing stands between.  The empty statements keep every
+// product of x in front of the wait and every read of its results behind.
 template <class T, int N>
 __device__ __forceinline__ void at_products_done(T (&x)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
-  asm volatile("s_nop 7\n\ts_nop 2");
+  if constexpr (sizeof(T) == sizeof(at_f32x4))
+    asm volatile("s_nop 7");
+  else
+    asm volatile("s_nop 7\n\ts_nop 3");
 #pragma unroll
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
 }
