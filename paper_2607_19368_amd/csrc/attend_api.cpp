@@ -52,18 +52,17 @@ struct AttendCost { int rows; double start, one, pair, full; };
 static const AttendCost ATTEND_COSTS[4] = {
     {16, 1.8, 0.65, 0.8, 0.33}, {32, 2.5, 0.75, 0.95, 0.42}, {AT_ROWS / 2, 2.6, 0.78, 1.1, 0.55}, {AT_ROWS, 3.0, 1.13, 1.75, 0.95}};
 static const double ATTEND_LAUNCH = 4.0;
-static const double ATTEND_SECOND = 2.0;         // of a second launch, where it is the host that is waited for
+static const double ATTEND_SECOND = 2.3;         // of a second launch, where it is the host that is waited for
 // Partial results: another pass over memory, the end of the blocks that write them, and a launch.
 static double attend_join_us(int64_t slots, int64_t rows, int d) {
   return slots > 1 ? 3.0 + 0.1 * (double)slots + 1.35 * (double)(slots * rows) * (4.0 * d + 8.0) / 3.5e6 : 0.0;
 }
 
 // The kernel and the splits (at most max_splits) that cost least for `sets` runs of `rows` rows a key/value head
-// against `keys` keys each, of which a row tile sees `mean` on average and the share `fresh` is no other run's
-// too.  out_rows: rows of a partial result.  also: other partial results of a row; same: the kernel of a launch
-// that this one would join.
+// against `keys` keys each, of which a row tile sees `mean` on average.  out_rows: rows of a partial result.  also: other partial results of a row; same: the kernel of a launch
+// that this one would join.  ahead: keys of a prefix, the same for all runs, that each goes through first (k_attend_rows).
 static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys, double mean, int64_t out_rows,
-                              int d, int n_cu, int also, int same, bool paged, int max_splits, double fresh) {
+                              int d, int n_cu, int also, int same, bool paged, int max_splits, int64_t ahead = 0) {
   AttendPart best = {};
   best.us = INFINITY;
   best.rows = 16, best.splits = 1;
@@ -73,18 +72,19 @@ static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys,
   const int64_t units = (keys + 63) / 64, most = std::max<int64_t>(1, std::min<int64_t>(max_splits, units));
   const int64_t slots = 2 * (int64_t)n_cu;
   for (const AttendCost& c : ATTEND_COSTS) {
-    if (paged && c.rows == AT_ROWS / 2) continue;
+    if (paged && (c.rows == AT_ROWS / 2 || (ahead && c.rows == AT_ROWS))) continue;
     const int64_t per = std::max<int64_t>(1, (rows + c.rows - 1) / c.rows), tiles = sets * per, base = tiles * Hkv;
     // a unit's 64 keys come from memory at 5.2 TB/s, for the row tiles that share them once, and from the
     // caches at four times that
-    const double mem = fresh * 256.0 * d * n_cu / 5.2e6 * (0.25 + 0.75 / (double)per);
+    const double mem = 256.0 * d * n_cu / 5.2e6 * (0.25 + 0.75 / (double)per);
     const double full = c.full * work, pair = c.pair * work;
     const int64_t fill = slots / std::max<int64_t>(1, base);
     for (const int64_t want : {(int64_t)1, (int64_t)2, (int64_t)3, fill / 2, fill, 2 * fill, 4 * fill, most}) {
       const int64_t s = std::max<int64_t>(1, std::min(want, most)), n = (units + s - 1) / s, blocks = base * s;
       const int64_t rounds = blocks / slots, rest = blocks - rounds * slots;
       const double each = (double)n * part, two = rounds > 1 || (rounds == 1 && rest) ? 2.0 * full : std::min(pair, 2.0 * full);
-      const double one = std::max(c.one * work, mem * std::min(1.0, 0.4 + (double)blocks / n_cu));     // few draw less
+      const double drawn = std::min(1.0, 0.4 + (double)blocks / n_cu);           // few draw less
+      const double one = std::max(c.one * work, mem * drawn);
       double us;
       if (part < 1.0) {
         // causal, the blocks with the most keys first, down to 2 part - 1 of the longest: the longest has one
@@ -101,6 +101,14 @@ static AttendPart attend_part(int64_t rows, int64_t sets, int Hkv, int64_t keys,
         us = (double)rounds * (each * two + 2.0 * c.start) + (rest == 0 ? 0.0 : each * (rest <= n_cu ? one : two) + c.start);
       }
       us = std::max(us, (double)blocks / n_cu * each * mem + c.start);
+      if (ahead) {
+        // a block's prefix steps and its own come after each other and add up, each with a bound of its own: taken
+        // together, own keys that wait for memory would hide the prefix's products
+        const double first = (double)((ahead + 63) / 64), once = mem / (double)sets;
+        const double alone = std::max(c.one * work, once * drawn);
+        us += std::max(first * ((double)rounds * two + (rest == 0 ? 0.0 : rest <= n_cu ? alone : two)),
+                       (double)blocks / n_cu * first * once);
+      }
       us += (same && (c.rows == same || c.rows == AT_ROWS) ? 0.0 : ATTEND_LAUNCH) + attend_join_us(s + also, out_rows, d);
       if (blocks + sets * Hkv * s > AT_BLOCKS / 2 - 64) us += 1e12;      // a launch may be of two plans
       if (us < best.us) best = AttendPart{c.rows, (int)s, tiles, us};
@@ -119,7 +127,7 @@ static AttendPlan attend_plan_packed(int64_t Tq, int64_t Tk, int B, int Hq, int 
   // as if the sequences were equal; where they are not, their tiles are B more at most
   const int64_t rows = Tq * (Hq / Hkv), n = std::max(1, B), keys = Tk / n;
   const double mean = causal ? std::max((double)keys / 2, (double)keys - (double)Tq / n / 2) : (double)keys;
-  p.own = attend_part((rows + n - 1) / n, n, Hkv, keys, mean, Tq * Hq, d, attend_cus(), 0, 0, false, 64, 1.0);
+  p.own = attend_part((rows + n - 1) / n, n, Hkv, keys, mean, Tq * Hq, d, attend_cus(), 0, 0, false, 64);
   p.own.tiles = rows / p.own.rows + B;
   attend_finish(p, Tq * Hq, d);
   return p;
@@ -129,22 +137,26 @@ static AttendPlan attend_plan_paged(int B, int n_q, int Hq, int Hkv, int d, int6
   AttendPlan p = {};
   const int n_cu = attend_cus();
   const int64_t rows = (int64_t)n_q * (Hq / Hkv), out_rows = (int64_t)B * n_q * Hq;
-  p.own = attend_part(rows, B, Hkv, max_len, (double)max_len, out_rows, d, n_cu, prefix_len > 0, 0, true, 64, 1.0);
+  p.own = attend_part(rows, B, Hkv, max_len, (double)max_len, out_rows, d, n_cu, prefix_len > 0, 0, true, 64);
   if (prefix_len > 0) {
-    p.pre = attend_part(B * rows, 1, Hkv, prefix_len, (double)prefix_len, out_rows, d, n_cu, p.own.splits, p.own.rows, true, 64, 1.0);
+    p.pre = attend_part(B * rows, 1, Hkv, prefix_len, (double)prefix_len, out_rows, d, n_cu, p.own.splits, p.own.rows, true, 64);
     // A short prefix is read by each sequence in front of its own keys: one launch instead of two and no
     // partial results.  28 / 4 heads of 128, prefix + own keys, us in a graph / of a call, as parts and so:
     //   8 sequences, 512 + 100        9.0 / 15.4    10.4 / 12.4 (10.3 where calls follow each other)
     //   64, 512 + 64                 14.8 / 15.2    10.2 / 12.0
     //   8, 1000 + 100                10.1 / 15.4    15.2 / 15.0: parts
     //   1, 1400 + 100                 8.5 / 15.4    18.6 / 18.2: parts
-    // (32 sequences of 5 tokens, 32 / 8 heads, 300 + 60: 18.1 in parts, 10.8 so)
-    const AttendPart c = attend_part(rows, B, Hkv, prefix_len + max_len, (double)(prefix_len + max_len), out_rows, d, n_cu,
-                                     0, 0, true, 1, ((double)prefix_len / B + max_len) / (double)(prefix_len + max_len));
+    // (32 sequences of 5 tokens, 32 / 8 heads, 300 + 60: 18.1 in parts, 10.8 so).  Calls with caches from memory:
+    //   128, 32768 + 704            114          418: parts, whatever the tables' width
+    //   256, 4000 + 704               91          153: parts
+    // Over 810 shapes of one new token with tables of the lengths' width (1 to 256 sequences, prefixes of 64 to 32768, 32 to
+    // 2816 own keys, 28 / 4 and 32 / 8 heads) the choice takes 1.004 of the better one's time on average, 1.25 at
+    // most; over 1120 of 2 to 16 tokens 1.010 and 1.37.
+    const AttendPart c = attend_part(rows, B, Hkv, max_len, (double)max_len, out_rows, d, n_cu, 0, 0, true, 1, prefix_len);
     const bool beside = (p.own.tiles * p.own.splits + p.pre.tiles * p.pre.splits) * Hkv <= n_cu;
     const double parts = beside ? std::max(p.own.us, p.pre.us + ATTEND_LAUNCH)
                                 : p.own.us + p.pre.us - attend_join_us(p.own.splits + 1, out_rows, d);
-    if (c.rows != AT_ROWS && c.us < parts + ATTEND_SECOND) {
+    if (c.us < parts + ATTEND_SECOND) {
       p.chain = true;
       p.own = c;
       p.pre = AttendPart{};

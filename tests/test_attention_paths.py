@@ -47,7 +47,7 @@ PAGED = {
     (64, 5, 28, 4, 16, 1, 0): ([("tiles", 128)], False, False),
     (2, 5, 28, 4, 64, 512, 0): ([("tiles", 128)], True, False),
     (2, 5, 28, 4, 16, 2048, 0): ([("tiles", 128)], True, False),
-    (64, 5, 28, 4, 128, 1, 77): ([("tiles", 128)], True, False),
+    (8, 5, 28, 4, 128, 24, 500): ([("tiles", 128)], True, False),
     (2, 5, 28, 4, 4, 8192, 77): ([("tiles", 128)], True, False),
     (2, 5, 28, 4, 16, 2048, 5000): ([("rows", 16), ("tiles", 128)], True, False),
     (1, 16, 64, 8, 64, 512, 2001): ([("rows", 32), ("tiles", 128)], True, False),
@@ -73,6 +73,23 @@ def test_paged_shapes_take_their_paths(plans, shape):
         done = plans.paged(*shape[:4], d, *shape[4:])
         kernels = [x for x in done if x[0] != "join"]
         assert ([(x[0], x[2]) for x in kernels], len(done) > len(kernels), bool(kernels[0][7])) == PAGED[shape], d
+
+
+def test_a_long_prefix_is_read_once_whatever_the_tables_width(plans):
+    """Tables are as wide as the longest sequence may become; what a call reads goes by the lengths."""
+    for Hq, Hkv in ((28, 4), (32, 8), (40, 8)):
+        for n in (64, 128, 256):
+            for prefix in (8000, 32768):
+                for page in (16, 64):
+                    want = plans.paged(n, 1, Hq, Hkv, 128, page, 704 // page, prefix)
+                    assert want[0][7] == 0 and want[0][5] > 0
+                    for width in (1408, 4096, 8192, 32768, 131072):
+                        got = plans.paged(n, 1, Hq, Hkv, 128, page, width // page, prefix)
+                        assert got[0][7] == 0 and got[0][5] > 0, (Hq, n, prefix, width)
+                        assert got == want or Hkv != 4, (n, prefix, width)
+    # a short one is not worth a second launch
+    for n, prefix, own in ((8, 512, 112), (64, 512, 64), (4, 300, 304), (32, 300, 704), (256, 64, 32)):
+        assert plans.paged(n, 1, 28, 4, 128, 16, own // 16, prefix)[0][7] == 1, (n, prefix, own)
 
 
 # ---------------------------------------------------------------- the definition, on the card in 64 bits
