@@ -480,7 +480,8 @@ int slh_merge_noalloc(const void *X, int32_t x_dtype, int64_t ldx, int64_t N, in
  *   SLH_ROPE_BANDS   f_i where it turns beta_fast times or more within orig_len tokens, f_i / factor
  *                    where beta_slow times or fewer, in between mixed linearly in the turns;
  *                    s = 0.1 ln(factor) + 1
- * rot_dim: a multiple of 16 from 16 to 256; base > 1; factor >= 1; 0 < beta_slow < beta_fast.
+ * rot_dim: a multiple of 16 from 16 to 256; n_pos rot_dim / 2 <= 2^32 - 256; base > 1; factor >= 1;
+ * 0 < beta_slow < beta_fast.
  */
 #define SLH_ROPE_PLAIN  0
 #define SLH_ROPE_LINEAR 1

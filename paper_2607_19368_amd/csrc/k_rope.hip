@@ -256,6 +256,8 @@ int slh_rope_table(float* table, int64_t n_pos, int32_t rot_dim, double base, in
       (orig_len < 1 || !(beta_slow > 0.0) || !(beta_fast > beta_slow) || std::isinf(beta_fast)))
     return SLH_EINVAL;
   const int half = rot_dim / 2;
+  const int64_t n = n_pos * half, blocks = (n + 255) / 256;
+  if (blocks * 256 > (int64_t)UINT32_MAX) return SLH_EINVAL;      // threads of a launch
   RopeFreqs fr = {};
   double mscale = 1.0;
   if (scaling == SLH_ROPE_BASE) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
@@ -270,9 +272,7 @@ int slh_rope_table(float* table, int64_t n_pos, int32_t rot_dim, double base, in
     fr.f[i] = f;
   }
   if (scaling == SLH_ROPE_BANDS) mscale = 0.1 * std::log(factor) + 1.0;
-  const int64_t n = n_pos * half, blocks = (n + 255) / 256;
   (void)hipGetLastError();
-  if (blocks > INT32_MAX) return SLH_EINVAL;
   hipLaunchKernelGGL(k_rope_table, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, table, n, half,
                      mscale, fr);
   return hipGetLastError() == hipSuccess ? SLH_OK : SLH_EHIP;
