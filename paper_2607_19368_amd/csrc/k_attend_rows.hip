@@ -43,12 +43,12 @@ hipError_t launch_attend_rows(const AttendArgs& a, bool paged, bool bf16, int ro
 // bytes a row and split, read once (128 tokens of 28 heads, up to 19 splits: 35 MB in 8.5 us;
 // 387 tokens of 40 heads, 4 splits: 32 MB in 11 us).
 template <class TY, int WAVES>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int slots) {
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int slots, int64_t row0) {
   constexpr int PARTS = 2 * WAVES;                 // half waves of a row
   __shared__ at_f32x4 s_o[WAVES == 1 ? 1 : WAVES * 32];
   const int lane = threadIdx.x & 63, half = lane >> 5, e = 4 * (lane & 31);
   const int wave = threadIdx.x >> 6, part = WAVES == 1 ? half : 2 * wave + half;
-  const int64_t r = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  const int64_t r = row0 + (WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x);
   if (r >= a.rows) return;
   const int64_t tok = r / a.Hq;
   const int h = (int)(r - tok * a.Hq);
@@ -121,16 +121,24 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int d, int sl
 
 hipError_t launch_attend_join(const AttendArgs& a, bool bf16, int d, int slots, hipStream_t s) {
   const bool wide = slots > 8 && a.rows <= 1024;
-  const dim3 grid((unsigned)(wide ? a.rows : (a.rows + 3) / 4)), block(256);
-  if (bf16 && wide)
-    hipLaunchKernelGGL((k_attend_join<AtBf16, 4>), grid, block, 0, s, a, d, slots);
-  else if (bf16)
-    hipLaunchKernelGGL((k_attend_join<AtBf16, 1>), grid, block, 0, s, a, d, slots);
-  else if (wide)
-    hipLaunchKernelGGL((k_attend_join<AtF16, 4>), grid, block, 0, s, a, d, slots);
-  else
-    hipLaunchKernelGGL((k_attend_join<AtF16, 1>), grid, block, 0, s, a, d, slots);
-  return hipGetLastError();
+  const dim3 block(256);
+  // a launch has fewer than 2^32 threads: 2^25 rows, a wave each, at a time
+  constexpr int64_t MOST = (int64_t)1 << 25;
+  for (int64_t row0 = 0; row0 < a.rows; row0 += MOST) {
+    const int64_t rows = a.rows - row0 < MOST ? a.rows - row0 : MOST;
+    const dim3 grid((unsigned)(wide ? rows : (rows + 3) / 4));
+    if (bf16 && wide)
+      hipLaunchKernelGGL((k_attend_join<AtBf16, 4>), grid, block, 0, s, a, d, slots, row0);
+    else if (bf16)
+      hipLaunchKernelGGL((k_attend_join<AtBf16, 1>), grid, block, 0, s, a, d, slots, row0);
+    else if (wide)
+      hipLaunchKernelGGL((k_attend_join<AtF16, 4>), grid, block, 0, s, a, d, slots, row0);
+    else
+      hipLaunchKernelGGL((k_attend_join<AtF16, 1>), grid, block, 0, s, a, d, slots, row0);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace slh

@@ -4,6 +4,7 @@ import torch
 
 import paper_2607_19368_amd as P
 from paper_2607_19368_amd import slh as B
+from test_attention_paths import close, rows_of
 
 gpu = pytest.mark.gpu
 
@@ -24,3 +25,26 @@ def test_a_table_at_the_limit():
     for p in (0, 1, n // 2, n - 1):
         a = p * f
         assert float((table[p].cpu().double() - torch.stack([a.cos(), a.sin()])).abs().max()) <= 2.0 ** -24 + n * 2.0 ** -51, p
+
+
+@gpu
+def test_partial_results_of_more_rows_than_a_launch_has_threads_for():
+    """2^26 rows, a wave each, are 2^32 threads."""
+    n, Hq, d, page, prefix = 2 ** 16, 1024, 64, 16, 600
+    assert P.slh_attend_paged_workspace(n, 1, Hq, 1, d, page, prefix) >= 2 * n * Hq * (4 * d + 8)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    n_pre = -(-prefix // page)
+    kc, vc = (torch.randn(n_pre + n, 1, page, d, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(1, 1024, d, generator=g, device="cuda").to(torch.bfloat16).repeat(n, 1, 1)
+    table = (n_pre + torch.arange(n, dtype=torch.int32, device="cuda"))[:, None]
+    lens = (torch.arange(n, dtype=torch.int32, device="cuda") % page) + 1
+    pre = torch.arange(n_pre, dtype=torch.int32, device="cuda")
+    lse = torch.full((n, Hq), 7.0, device="cuda")
+    out = P.slh_attend_paged(q, kc, vc, table, lens, pre, prefix, lse_out=lse)
+    shared = [x[:n_pre, 0].reshape(-1, 1, d)[:prefix] for x in (kc, vc)]
+    for b in (0, 1, n // 2 - 1, n // 2, n // 2 + 1, n - 2, n - 1):
+        k, v = (torch.cat([s, x[n_pre + b, 0, :int(lens[b]), None]]) for s, x in zip(shared, (kc, vc)))
+        o, tol, e, etol = rows_of(q[b:b + 1], k, v, [len(k)], d ** -0.5)
+        close(out[b:b + 1], o, tol, f"sequence {b}")
+        assert bool(((lse[b:b + 1].double() - e).abs() <= etol).all())
