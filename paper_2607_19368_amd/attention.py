@@ -1,6 +1,7 @@
 """Python binding of the operators behind a compressed prompt (include/slh.h): argument
 checks and marshalling, as in slh.py.  Every call goes to torch's current stream, or to the
-`stream` given (a torch.cuda.Stream), and returns without waiting for it.
+`stream` given (a torch.cuda.Stream), and returns without waiting for it.  The operators have no backward passes:
+tensors that require a gradient are refused where torch records one.
 """
 import math
 
@@ -18,6 +19,11 @@ _HALVES = (torch.bfloat16, torch.float16)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_recording = torch.is_grad_enabled
+
+
+def _no_gradient(name):
+    raise SLHError(f"{name} requires a gradient, and the operator has no backward pass: detach it or call under torch.no_grad()")
 
 
 def _call(name, dev, stream, args):
@@ -40,6 +46,8 @@ def _first(name, t, dims):
         raise SLHError(f"{name} must be a device tensor")
     if t.dtype not in _DTYPES:
         raise SLHError(f"{name}: unsupported type {t.dtype}")
+    if t.requires_grad and _recording():
+        _no_gradient(name)
     shape, st = t.shape, t.stride()
     if len(shape) not in dims or (st[-1] != 1 and t.numel() > 0):
         raise SLHError(f"{name} must have {' or '.join(map(str, dims))} dimensions and unit stride in the last")
@@ -52,6 +60,8 @@ def _rows(name, t, dtype, dev, shape):
         raise SLHError(f"{name} must be a {dtype} tensor on device {dev}")
     if t.shape != shape:
         raise SLHError(f"{name} must have shape {tuple(shape)}")
+    if t.requires_grad and _recording():
+        _no_gradient(name)
     st = t.stride()
     if st[-1] != 1 and t.numel() > 0:
         raise SLHError(f"{name} must have unit stride in the last dimension")
@@ -64,6 +74,8 @@ def _plain(name, t, dtype, dev, shape):
         raise SLHError(f"{name} must be a contiguous {dtype} tensor on device {dev}")
     if t.shape != shape if shape.__class__ is not int else t.dim() != shape:
         raise SLHError(f"{name} must have " + (f"{shape} dimensions" if isinstance(shape, int) else f"shape {tuple(shape)}"))
+    if t.requires_grad and _recording():
+        _no_gradient(name)
     return t.data_ptr()
 
 
