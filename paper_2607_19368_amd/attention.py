@@ -40,6 +40,11 @@ def _call(name, dev, stream, args):
             B.SLH_EHIP: "a kernel launch failed"}.get(rc, ""))
 
 
+def _strides(st, shape):
+    """Strides without those of single tokens and heads: they reach nothing, and torch leaves any value in them."""
+    return [0 if n == 1 else s for n, s in zip(shape, st)]
+
+
 def _first(name, t, dims):
     """(type, device index, shape, strides) of the tensor of rows that the others go by."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -49,6 +54,8 @@ def _first(name, t, dims):
     if t.requires_grad and _recording():
         _no_gradient(name)
     shape, st = t.shape, t.stride()
+    if 1 in shape and (shape[0] == 1 or shape[-2] == 1):
+        st = _strides(st, shape)
     if len(shape) not in dims or (st[-1] != 1 and t.numel() > 0):
         raise SLHError(f"{name} must have {' or '.join(map(str, dims))} dimensions and unit stride in the last")
     return t.dtype, t.get_device(), shape, st
@@ -56,13 +63,18 @@ def _first(name, t, dims):
 
 def _rows(name, t, dtype, dev, shape):
     """Strides of t, a tensor of rows with unit element stride."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev:
-        raise SLHError(f"{name} must be a {dtype} tensor on device {dev}")
+    try:
+        if t.dtype is not dtype or t.get_device() != dev:
+            raise SLHError(f"{name} must be a {dtype} tensor on device {dev}")
+    except AttributeError:
+        raise SLHError(f"{name} must be a tensor") from None
     if t.shape != shape:
         raise SLHError(f"{name} must have shape {tuple(shape)}")
     if t.requires_grad and _recording():
         _no_gradient(name)
     st = t.stride()
+    if 1 in shape and (shape[0] == 1 or shape[-2] == 1):
+        st = _strides(st, shape)
     if st[-1] != 1 and t.numel() > 0:
         raise SLHError(f"{name} must have unit stride in the last dimension")
     return st
@@ -70,8 +82,11 @@ def _rows(name, t, dtype, dev, shape):
 
 def _plain(name, t, dtype, dev, shape):
     """Address of t, a contiguous tensor of `shape`, or of so many dimensions."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
-        raise SLHError(f"{name} must be a contiguous {dtype} tensor on device {dev}")
+    try:
+        if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+            raise SLHError(f"{name} must be a contiguous {dtype} tensor on device {dev}")
+    except AttributeError:
+        raise SLHError(f"{name} must be a tensor") from None
     if t.shape != shape if shape.__class__ is not int else t.dim() != shape:
         raise SLHError(f"{name} must have " + (f"{shape} dimensions" if isinstance(shape, int) else f"shape {tuple(shape)}"))
     if t.requires_grad and _recording():
