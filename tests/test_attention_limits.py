@@ -48,3 +48,56 @@ def test_partial_results_of_more_rows_than_a_launch_has_threads_for():
         o, tol, e, etol = rows_of(q[b:b + 1], k, v, [len(k)], d ** -0.5)
         close(out[b:b + 1], o, tol, f"sequence {b}")
         assert bool(((lse[b:b + 1].double() - e).abs() <= etol).all())
+
+
+# ---------------------------------------------------------------- what lies in device memory
+@gpu
+@pytest.mark.parametrize("lk", [60, 5000])         # in one piece, and with the keys split
+def test_sequence_bounds_outside_the_tensors_are_taken_as_the_nearest(lk):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(lk)
+    q, k, v = (torch.randn(n, h, 64, generator=g, device="cuda").to(torch.bfloat16) for n, h in ((20, 4), (lk, 2), (lk, 2)))
+
+    def run(cq, ck):
+        out, lse = torch.full_like(q, 7.0), torch.full((20, 4), 7.0, device="cuda")
+        P.slh_attend(q, k, v, *(torch.tensor(x, dtype=torch.int32, device="cuda") for x in (cq, ck)), out=out, lse_out=lse)
+        return out, lse
+
+    low, high = -2 ** 31, 2 ** 31 - 1
+    for cq, ck in (([low, 7, high], [-1, 31, lk + 1]), ([-3, 20, 21], [low, lk + 9, high]), ([0, 9, 20], [low, low, high])):
+        near = [[min(max(x, 0), n) for x in c] for c, n in ((cq, 20), (ck, lk))]
+        for a, b in zip(run(cq, ck), run(*near)):
+            assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("n,n_q,prefix", [(3, 1, 40), (3, 2, 0), (3, 2, 3000), (40, 3, 3000)])
+def test_lengths_and_pages_outside_the_cache(n, n_q, prefix):
+    """Lengths are taken as the nearest that the table has room for; a page that is none spoils its own sequence alone; a
+    table without columns is one of lengths 0."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + prefix)
+    page, width, Hq, Hkv, d = 16, 5, 28, 4, 64
+    n_pre = -(-prefix // page)
+    kc, vc = (torch.randn(n_pre + n * width, Hkv, page, d, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    pre = torch.arange(n_pre, dtype=torch.int32, device="cuda")
+    table = (n_pre + torch.arange(n * width, dtype=torch.int32, device="cuda")).view(n, width)
+    q = torch.randn(n, n_q, Hq, d, generator=g, device="cuda").to(torch.bfloat16)
+
+    def run(lens, table=table):
+        lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        return P.slh_attend_paged(q, kc, vc, table, lens, pre, prefix)
+
+    most = page * width
+    lens = [(17 * b) % most for b in range(n)]
+    assert torch.equal(run([2 ** 31 - 1, -2 ** 31, -1] + lens[3:]), run([most, 0, 0] + lens[3:]))
+    want = run(lens)
+    for wrong in (-1, -2 ** 31, 2 ** 31 - 1, len(kc)):
+        spoiled = table.clone()
+        spoiled[1, 0] = wrong
+        got = run(lens, spoiled)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[2:], want[2:])
+    got = run([0] * n, table[:, :0])
+    for b in range(0, n, 7):
+        o, tol, _, _ = rows_of(q[b], *(x[:n_pre].permute(0, 2, 1, 3).reshape(-1, Hkv, d)[:prefix] for x in (kc, vc)), [prefix] * n_q, d ** -0.5)
+        close(got[b], o, tol, f"sequence {b}")
