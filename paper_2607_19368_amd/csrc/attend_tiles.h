@@ -26,9 +26,10 @@
 // compute unit, so that one's softmax runs beside the other's products; the next tile goes straight to the
 // other LDS buffer while one is worked on, its loads asked for a few at a time behind the products (all at
 // once at the barrier: 16384 causal tokens 2.61 instead of 2.51 ms).
-// Measured, bf16, d = 128: one causal prompt of 16384 tokens, 40 / 8 heads, 2.54 ms = 1084 TFLOP/s, where
-// an 8192^3 library product of the same random numbers reaches 1113; with zeros for inputs 1283, for then
-// the power limit leaves the clock alone.  23 causal sequences of 59 to 1458 tokens, 32 / 8 heads, 138 us = 660 TFLOP/s:
+// Measured, bf16, d = 128: one causal prompt of 16384 tokens, 40 / 8 heads, 2.50 to 2.70 ms on different cards = 1100 to
+// 1018 TFLOP/s, where an 8192^3 library product of the same random numbers reaches 1113 on the card on which this took 2.54; with
+// zeros for inputs 1283.  The matrix units are busy for 57 % of the cycles, at 1.75 GHz: the power limit lowers the clock,
+// and the rest of a tile's time is its softmax.  23 causal sequences of 59 to 1458 tokens, 32 / 8 heads, 136 us = 667 TFLOP/s:
 // of a block's 23 us, 7 are its task, first loads and last stores, and 10 % of the products are masked.
 #pragma once
 #include "attend.h"
@@ -96,6 +97,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
   // tiles of this split
   const int all = (end + AT_KEYS - 1) / AT_KEYS, each = (all + t.n_split - 1) / t.n_split;
   const int t0 = min(all, t.split * each), t1 = min(all, t0 + each);
+  const bool empty = t0 >= t1 || limit <= t0 * AT_KEYS;      // the row sees none of these keys
 
   at_u32x4 qf[KS];
   {
@@ -403,7 +405,6 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
         for (int f = 0; f < 4; ++f) o[b][e + f] = __builtin_fmaf(k1, o[b][e + f], k2 * x[f]);
       }
   }
-  const bool empty = t0 >= t1 || limit <= t0 * AT_KEYS;      // sees none of this split's keys
   const int64_t r = (t.tok0 + i) * a.Hq + h;
   if (a.part_o) {
     if (!real) return;
