@@ -18,6 +18,7 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import paper_2607_19368_amd as P  # noqa: E402
+from paper_2607_19368_amd import slh as B  # noqa: E402
 
 PAGE = 16
 # query and key/value heads of 128 elements of the workloads' models
@@ -63,21 +64,31 @@ def decode(layer, x, pos, cache, table, lens, pages, M):
     return P.slh_attend_paged(q, *cache, table, lens, pages, M)
 
 
-def run(X, ctx, n_it, layer, questions):
-    """Compresses X [N, D], prefills the layer with its macro-tokens and decodes questions [B, n, D].
-    Returns (E, positions, prefill output [M, Hq, d], decode outputs [B, n, Hq, d])."""
+def context(wl):
+    """A context for prompts of a workload, with its windows, preserved suffix, operator and exact length."""
+    ctx = P.slh_create(wl.N, wl.D, wl.m, wl.r, wl.bits, 0)
+    for key, value in ((B.SLH_OPT_KEEP_LAST, wl.keep_last), (B.SLH_OPT_WINDOW_LEN, wl.window),
+                       (B.SLH_OPT_NORMALIZE, int(wl.normalise)), (B.SLH_OPT_TARGET_LEN, wl.target)):
+        if value:
+            P.slh_set_option(ctx, key, value)
+    return ctx
+
+
+def run(X, ctx, n_it, layer, questions, rho=None):
+    """Compresses X [N, D] (rho: routed, as P.compress), prefills the layer with its macro-tokens and decodes questions
+    [n_seq, n, D].  Returns (E, positions, prefill output [M, Hq, d], decode outputs [n_seq, n, Hq, d])."""
     N = X.shape[0]
-    E, pos, _, M, _ = P.compress(ctx, X, n_it)
-    B, n, _ = questions.shape
+    E, pos, _, M, _ = P.compress(ctx, X, n_it, rho)
+    n_seq, n, _ = questions.shape
     n_pre, n_own = -(-M // PAGE), -(-n // PAGE)
-    cache = [torch.empty((n_pre + B * n_own, layer.Hkv, PAGE, layer.d), dtype=torch.bfloat16, device=X.device) for _ in range(2)]
+    cache = [torch.empty((n_pre + n_seq * n_own, layer.Hkv, PAGE, layer.d), dtype=torch.bfloat16, device=X.device) for _ in range(2)]
     pages = torch.arange(n_pre, dtype=torch.int32, device=X.device)
-    table = (n_pre + torch.arange(B * n_own, dtype=torch.int32, device=X.device)).view(B, n_own)
+    table = (n_pre + torch.arange(n_seq * n_own, dtype=torch.int32, device=X.device)).view(n_seq, n_own)
     out = prefill(layer, E, pos, cache, pages)
-    lens = torch.zeros(B, dtype=torch.int32, device=X.device)
+    lens = torch.zeros(n_seq, dtype=torch.int32, device=X.device)
     steps = []
     for t in range(n):
-        at = torch.full((B,), N + t, dtype=torch.int32, device=X.device)     # behind the whole document
+        at = torch.full((n_seq,), N + t, dtype=torch.int32, device=X.device)     # behind the whole document
         steps.append(decode(layer, questions[:, t], at, cache, table, lens, pages, M))
     return E, pos, out, torch.stack(steps, 1)
 
@@ -85,25 +96,26 @@ def run(X, ctx, n_it, layer, questions):
 def main():
     from workloads import make_inputs
     name = sys.argv[1] if len(sys.argv) > 1 else "qwen7b"
-    B = int(sys.argv[2]) if len(sys.argv) > 2 else 16
+    n_seq = int(sys.argv[2]) if len(sys.argv) > 2 else 16
     n = int(sys.argv[3]) if len(sys.argv) > 3 else 8
     inp = make_inputs(name)
     wl = inp.workload
     X = torch.from_numpy(inp.X if inp.X.dtype == "float32" else inp.X.view("int16"))
     X = X.cuda() if X.dtype == torch.float32 else X.view(torch.bfloat16).cuda()
-    ctx = P.slh_create(wl.N, wl.D, wl.m, wl.r, wl.bits, 0)
+    ctx = context(wl)
+    rho = wl.rho if wl.adaptive else None
     layer = Layer(wl.D, *HEADS[wl.D], n_pos=wl.N + n)
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
-    questions = torch.randn((B, n, wl.D), generator=g, device="cuda") * 0.02
-    run(X, ctx, wl.n_it, layer, questions)
+    questions = torch.randn((n_seq, n, wl.D), generator=g, device="cuda") * 0.02
+    run(X, ctx, wl.n_it, layer, questions, rho)
     torch.cuda.synchronize()
     t = time.perf_counter()
-    E, pos, out, steps = run(X, ctx, wl.n_it, layer, questions)
+    E, pos, out, steps = run(X, ctx, wl.n_it, layer, questions, rho)
     torch.cuda.synchronize()
     ms = (time.perf_counter() - t) * 1e3
     print(f"{name}: {wl.N} tokens -> {len(E)} macro-tokens at positions 0..{int(pos[-1])}; prefill {tuple(out.shape)}, "
-          f"{B} questions of {n} tokens {tuple(steps.shape)}: {ms:.2f} ms in all")
+          f"{n_seq} questions of {n} tokens {tuple(steps.shape)}: {ms:.2f} ms in all")
 
 
 if __name__ == "__main__":

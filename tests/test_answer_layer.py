@@ -48,3 +48,20 @@ def test_answers_behind_a_compressed_prompt():
             vv = torch.cat([v] + [r[2][b:b + 1] for r in own])
             o, tol, _, _ = AP.attend(own[t][0][b:b + 1], kk, vv, [M + t + 1], scale)
             assert bool(((steps[b, t].double().cpu() - o[0]).abs() <= tol[0]).all()), (b, t)
+
+
+@pytest.mark.parametrize("name", ["local16", "qwen7b_exact"])
+def test_workloads_are_run_with_their_options(name):
+    """Windows, preserved suffix and exact length are the workload's."""
+    inp = make_inputs(name)
+    wl = inp.workload
+    ctx = AL.context(wl)
+    layer = AL.Layer(wl.D, *AL.HEADS[wl.D], n_pos=wl.N + 1)
+    asked = torch.zeros((2, 1, wl.D), device="cuda")
+    E, pos, out, _ = AL.run(PR.to_device_x(inp), ctx, wl.n_it, layer, asked)
+    assert len(out) == len(E) == len(pos)
+    if wl.target:
+        assert len(E) == wl.target
+    if wl.window:
+        assert ctx.n_windows == (wl.N - wl.keep_last) // wl.window and len(E) >= ctx.n_windows + wl.keep_last
+        assert pos[-wl.keep_last:].tolist() == list(range(wl.N - wl.keep_last, wl.N))
