@@ -479,7 +479,10 @@ int slh_merge_noalloc(const void *X, int32_t x_dtype, int64_t ldx, int64_t N, in
  *   SLH_ROPE_BASE    base factor^(rot_dim / (rot_dim - 2)) in the place of base
  *   SLH_ROPE_BANDS   f_i where it turns beta_fast times or more within orig_len tokens, f_i / factor
  *                    where beta_slow times or fewer, in between mixed linearly in the turns;
- *                    s = 0.1 ln(factor) + 1
+ *                    s = 0.1 ln(factor) + 1: the interpolation by parts of "YaRN: Efficient Context
+ *                    Window Extension of Large Language Models" (Peng et al., 2023), with its s.  A model
+ *                    trained with a mix that is linear in i, or with s = 1, needs a table of its own
+ *                    making: the operators below read any
  * rot_dim: a multiple of 16 from 16 to 256; n_pos rot_dim / 2 <= 2^32 - 256; base > 1; factor >= 1;
  * 0 < beta_slow < beta_fast.
  */

@@ -116,7 +116,7 @@ def _rotation(table, pos, T, dev):
 def slh_rope_table(n_pos, rot_dim, base=10000.0, scaling=B.SLH_ROPE_PLAIN, factor=1.0, orig_len=0,
                    beta_fast=32.0, beta_slow=1.0, device="cuda", stream=None):
     """Table [n_pos, 2, rot_dim / 2] float32 of cosines and sines for slh_qk_norm_rope and
-    slh_kv_append; `scaling` is one of SLH_ROPE_PLAIN, _LINEAR, _BASE and _BANDS."""
+    slh_kv_append; `scaling` is one of SLH_ROPE_PLAIN, _LINEAR, _BASE and _BANDS (include/slh.h)."""
     if n_pos < 1 or rot_dim < 16 or rot_dim > 256 or rot_dim % 16:
         raise SLHError("n_pos must be positive and rot_dim a multiple of 16 from 16 to 256")
     table = _empty((n_pos, 2, rot_dim // 2), torch.float32, device, stream)
@@ -211,7 +211,8 @@ def slh_attend(q, k, v, cu_q, cu_k=None, scale=None, causal=True, out=None, lse_
     """Attention of packed sequences: q [Tq, Hq, d], k and v [Tk, Hkv, d] (bf16 or fp16), sequence b
     at rows cu_q[b]..cu_q[b + 1] of q and cu_k[b]..cu_k[b + 1] of k and v (int32; cu_k None: as cu_q).
     causal: a sequence's last query sees all its keys, the one before it one fewer, and so on.
-    scale: 1 / sqrt(d) by default.  lse_out: [Tq, Hq] float32.  Returns out."""
+    scale: 1 / sqrt(d) by default.  lse_out: [Tq, Hq] float32.  Returns out; its rows of no sequence (in front of cu_q[0],
+    behind the last entry) are not written, so hold anything in a new one."""
     dtype, dev, shape, qs = _first("q", q, (3,))
     if dtype not in _HALVES:
         raise SLHError("q must be bfloat16 or float16")

@@ -40,8 +40,9 @@ struct AttendPlan {
 // of a block, for finding its rows and keys, its first loads and its last stores (and ATTEND_LAUNCH of the launch);
 // `one`: a block's 64 keys where it has a compute unit to itself; `pair`: where another block is beside
 // it; `full`: a unit's 64 keys of one block with all units busy for several rounds (power and caches are shared then).
-// Over 53 packed shapes (16 to 10000 tokens, 0 to 9000 keys in front) the plan's time is on average 1.02 of the best
-// of all kernels and 1 to 32 splits, over 45 paged ones 1.03.  One split, us, queries x context, heads:
+// Over 62 packed shapes (16 to 10000 tokens, 0 to 9000 keys in front) the plan's time is on average 1.02 of the best
+// of all kernels and 1 to 32 splits, over 45 paged ones 1.04 (sequences of equal lengths, tables as wide as those).  One
+// split, us, queries x context, heads:
 //                            16 rows   32 rows   64 rows   128 rows
 //   256 x 0, 28 / 4            7.3       9.0       8.8      10.4
 //   512 x 0, 28 / 4           15.3      12.7      12.3      15.4

@@ -12,9 +12,11 @@
 // a sequence's own.
 //
 // Measured, d = 128: two new tokens of 6 sequences of up to 49159 fp16 rows in pages of 32, 32 / 8 heads:
-// 987 MB in 175 us = 5.6 TB/s (180 with the join; a pure read of large buffers reaches 6.55 TB/s, a copy 4.75).  512 causal
+// 987 MB in 179 us = 5.5 TB/s, and 5 us of the join (a call 180.5; a pure read of large buffers reaches 6.55 TB/s, a copy 4.75).  512 causal
 // bf16 tokens, 28 / 4 heads: 12.7 us, the dependent chain of 8 steps of 0.6 us behind the launch.  8 sequences of 97
-// rows behind 512, 28 / 4 heads: 10.3 us, 10 such steps.
+// rows behind 512, 28 / 4 heads: 10.5 us, 10 such steps.
+//
+// Rounding to fewer bits: as in attend_tiles.h, the weights only, for the second product.
 #pragma once
 #include "attend.h"
 

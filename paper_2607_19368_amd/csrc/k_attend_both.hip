@@ -5,8 +5,8 @@
 //
 // 128 sequences, 28 / 4 heads of 128, a prefix of 32768 rows and up to 641 own, bf16, us with the join: two
 // launches 107, prefix first 101, own keys first 101, eights of both kinds alternating 144 (a unit that holds one
-// of each has too few waves of either).  With the loads spread as in attend_tiles.h: 94, of which
-// this kernel 84.5, the join 8.5.
+// of each has too few waves of either).  With the loads spread as in attend_tiles.h: 93, of which
+// this kernel 84.3, the join 8.5.
 #include "attend_rows.h"
 #include "attend_tiles.h"
 
