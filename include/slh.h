@@ -576,6 +576,99 @@ int slh_attend_paged(const void *q, int64_t q_st, int64_t q_sh, const void *k_ca
                      double scale, void *out, int64_t o_st, int64_t o_sh, float *lse,
                      void *workspace, int64_t workspace_bytes, void *stream);
 
+/*
+ * A smaller cache: held in 8 bits, and cut to the rows that received the most attention.  As above: no context, nothing
+ * kept, no waiting; what lies in device memory is kept in bounds by the kernels.
+ *
+ * A cache in 8 bits: k_cache, v_cache [n_pages][H][page_size][d] bytes of e4m3 codes (four exponent and three mantissa bits, no
+ * infinities), k_scale, v_scale [n_pages][H][page_size / block] bytes s.  A code stands for code 2^(s - 127), s from 1 to 254.
+ * page_size and block: powers of two, 16 <= block <= 256, block <= page_size <= 65536; n_pages H page_size < 2^31; d: 64,
+ * 80, 96 or 128; caches aligned to 16 bytes.  Pages belong to one sequence, unless they are only read (a shared prefix).
+ */
+
+/*
+ * New keys and values into a cache in 8 bits, the keys normed and rotated on the way as in slh_qk_norm_rope.  Tokens
+ * cu[b] <= t < cu[b + 1] of k and v (device, B + 1 entries, ascending, entries outside [0, T] taken as the nearest;
+ * NULL: T / B tokens each) become the last of the lens[b] rows of sequence b (the new rows counted; values outside [0, max_pages
+ * page_size] taken as the nearest; the first tokens of a sequence with more of them than rows are left out), in its pages
+ * page_table[b ld_pages + i] (max_pages entries; rows of pages outside [0, n_pages) are left out).
+ * Each block of rows, page and head gets the smallest power of two 2^x with max |new rows| <= 448 2^x, x >= -126, and at least
+ * the power that it has where earlier rows of the sequence are in it; those are then rescaled, exactly but for codes that
+ * become subnormal.  Codes are value 2^-x rounded to nearest even, from fp32.  Infinities and NaN count as no
+ * magnitude and become NaN.  Powers go up to 2^8 (dtype SLH_F16) or 2^120 (SLH_BF16, SLH_F32), with which codes up to
+ * 240 are used, so that every value that is held is finite in dtype.
+ * T H < 2^26; B <= 2^20; max_pages page_size < 2^29.
+ */
+int slh_kv_append_e4m3(const void *k, int64_t k_st, int64_t k_sh, const void *v, int64_t v_st,
+                       int64_t v_sh, int32_t dtype, int64_t T, int32_t B, int32_t H, int32_t d,
+                       const void *k_weight, double eps, const float *table, int64_t n_pos,
+                       int32_t rot_dim, const int32_t *pos, int32_t interleaved, void *k_cache,
+                       void *v_cache, void *k_scale, void *v_scale, int64_t n_pages,
+                       int32_t page_size, int32_t block, const int32_t *page_table,
+                       int64_t ld_pages, int32_t max_pages, const int32_t *lens, const int32_t *cu,
+                       void *stream);
+
+/*
+ * slh_attend_paged against a cache in 8 bits: its sequences, prefix, limits and results, with the codes' values as
+ * keys and values.  They are taken into the products in dtype (exact where they lie in its normal range; fp16: magnitudes from
+ * 65520 become infinite).  NaN codes that a query does not see do not reach it.
+ * workspace: slh_attend_paged_e4m3_workspace() bytes, with max_len = max_pages page_size.
+ */
+int64_t slh_attend_paged_e4m3_workspace(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d,
+                                        int64_t max_len, int64_t prefix_len);
+int slh_attend_paged_e4m3(const void *q, int64_t q_st, int64_t q_sh, const void *k_cache,
+                          const void *v_cache, const void *k_scale, const void *v_scale,
+                          int32_t dtype, int64_t n_pages, int32_t page_size, int32_t block,
+                          int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d,
+                          const int32_t *page_table, int64_t ld_pages, int32_t max_pages,
+                          const int32_t *lens, const int32_t *prefix_pages, int64_t prefix_len,
+                          double scale, void *out, int64_t o_st, int64_t o_sh, float *lse,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * The attention weight that each cached key received, added up:
+ *   weights[b][h][j] += sum over the queries i of sequence b that see row j and the query heads of key/value head h of
+ *                       exp(scale q_i . k_j - lse_i)
+ * for rows j < lens[b] (weights of others are left alone).  Queries cu_q[b] <= t < cu_q[b + 1] of q (device, B + 1 entries as for
+ * slh_attend; NULL: Tq / B each) are sequence b's; query i of n sees the first lens[b] - n + i + 1 rows.  lse: [Tq][Hq], as
+ * slh_attend or slh_attend_paged gave it for the same queries (over all that they saw, a prefix too); a query whose
+ * lse is -inf gives nothing.  k_cache: pages as slh_kv_append writes them, of dtype (SLH_BF16 or SLH_F16; page_size a power of two up to
+ * 65536), or, with k_scale, in 8 bits.  weights: [B][Hkv][max_pages page_size] floats.  Sums are fp32, in an order that
+ * is the same every call.  lens, page_table, heads, d, scale and strides as for slh_attend_paged.
+ * workspace: slh_attend_weights_workspace() bytes, with max_len = max_pages page_size.
+ * Limits: as for slh_attend_paged, and B Hkv (max_len / 128 + 1) <= 2^23.
+ */
+int64_t slh_attend_weights_workspace(int64_t Tq, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                     int64_t max_len);
+int slh_attend_weights(const void *q, int64_t q_st, int64_t q_sh, const void *k_cache,
+                       const void *k_scale, int32_t dtype, int64_t n_pages, int32_t page_size,
+                       int32_t block, int64_t Tq, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                       const int32_t *page_table, int64_t ld_pages, int32_t max_pages,
+                       const int32_t *lens, const int32_t *cu_q, const float *lse, double scale,
+                       float *weights, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Eviction: each sequence b with lens[b] > budget rows (lens outside [0, max_pages page_size] taken as the nearest) is cut to
+ * `budget` of them, for each head by itself: its first `first` and last `last` rows stay, and of the others those with the largest
+ * weights (equal ones: the first rows; zeros of both signs are equal; NaN counts as the largest).  What stays moves
+ * in its order to the first rows of the sequence's pages; rows behind are as they were.  kept[b][h][i] (device, [B][H][budget])
+ * says which row became row i, -1 where there is none.  weights_out: the weights of the rows as they are now, 0 behind
+ * the last.  lens_out[b] = min(lens[b], budget).  weights_out may be weights, lens_out lens.
+ * Caches of dtype (SLH_BF16, SLH_F16, SLH_F32; any d of slh_kv_append, page_size a power of two up to 65536), or, with k_scale and
+ * v_scale, in 8 bits (dtype is not looked at): the blocks of a sequence that is cut get the smallest power
+ * of two for the rows they now hold (at least 2^-126), the codes follow, exactly but for those that become subnormal.
+ * Rows of pages outside [0, n_pages) are not read or written.  budget >= 1; first + last <= budget;
+ * B H <= 2^23; max_pages page_size < 2^29.  workspace: slh_kv_evict_workspace() bytes (aligned to 16), which no other call
+ * may use until this one has run.
+ */
+int64_t slh_kv_evict_workspace(int32_t B, int32_t H);
+int slh_kv_evict(void *k_cache, void *v_cache, void *k_scale, void *v_scale, int32_t dtype,
+                 int64_t n_pages, int32_t page_size, int32_t block, int32_t B, int32_t H, int32_t d,
+                 const int32_t *page_table, int64_t ld_pages, int32_t max_pages,
+                 const int32_t *lens, int32_t *lens_out, const float *weights, float *weights_out,
+                 int32_t budget, int32_t first, int32_t last, int32_t *kept, void *workspace,
+                 int64_t workspace_bytes, void *stream);
+
 /* Number of windows and of spectral windows of the current routing. */
 int64_t slh_num_windows(const slh_ctx *ctx);
 int64_t slh_num_spectral(const slh_ctx *ctx);

@@ -6,21 +6,27 @@ from .slh import (  # noqa: F401
     slh_copy_out, slh_load, slh_stage_times, slh_time_passes, slh_spectral_energy, slh_bucket_purity, slh_eigh_ritz, slh_peak_read, slh_peak_mfma, slh_merge_noalloc, compress,
 )
 
-# The attention operators' binding is loaded when one of them is first asked for: it needs torch, the host calls above
+# The attention operators' bindings are loaded when one of them is first asked for: they need torch, the host calls above
 # do not.
 _ATTENTION = (
     "slh_rope_table", "slh_qk_norm_rope", "slh_kv_append", "slh_attend_workspace", "slh_attend",
     "slh_attend_paged_workspace", "slh_attend_paged",
 )
-__all__ = [n for n in globals() if not n.startswith("_")] + ["attention", *_ATTENTION]
+_CACHE = (
+    "slh_kv_append_e4m3", "slh_attend_paged_e4m3_workspace", "slh_attend_paged_e4m3", "slh_attend_weights_workspace",
+    "slh_attend_weights", "slh_kv_evict_workspace", "slh_kv_evict",
+)
+_LATER = {"attention": _ATTENTION, "cache": _CACHE}
+__all__ = [n for n in globals() if not n.startswith("_")] + [*_LATER, *_ATTENTION, *_CACHE]
 
 
 def __getattr__(name):
-    if name != "attention" and name not in _ATTENTION:
+    of = next((m for m, names in _LATER.items() if name == m or name in names), None)
+    if of is None:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
     from importlib import import_module
-    module = import_module(".attention", __name__)
-    globals().update({n: getattr(module, n) for n in _ATTENTION})
+    module = import_module("." + of, __name__)
+    globals().update({n: getattr(module, n) for n in _LATER[of]})
     return globals()[name]
 
 

@@ -37,6 +37,11 @@ SOURCES = [
     "k_attend_rows.hip",
     "k_attend_both.hip",
     "attend_api.cpp",
+    "k_append8.hip",
+    "k_rows8.hip",
+    "attend8_api.cpp",
+    "k_weights.hip",
+    "k_evict.hip",
 ]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

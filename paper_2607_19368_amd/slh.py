@@ -34,6 +34,8 @@ EXPORTS = [
     "slh_merge_async", "slh_merge_wait", "slh_operator_rows",
     "slh_rope_table", "slh_qk_norm_rope", "slh_kv_append", "slh_attend_workspace", "slh_attend",
     "slh_attend_paged_workspace", "slh_attend_paged",
+    "slh_kv_append_e4m3", "slh_attend_paged_e4m3_workspace", "slh_attend_paged_e4m3", "slh_attend_weights_workspace",
+    "slh_attend_weights", "slh_kv_evict_workspace", "slh_kv_evict",
 ]
 
 _lib = None
@@ -93,6 +95,17 @@ def load():
         "slh_attend_paged_workspace": (i64, [i32, i32, i32, i32, i32, i64, i64]),
         "slh_attend_paged": (i32, [vp, i64, i64, vp, vp, i32, i64, i32, i32, i32, i32, i32, i32, vp, i64, i32, vp,
                                    vp, i64, f64, vp, i64, i64, vp, vp, i64, vp]),
+        "slh_kv_append_e4m3": (i32, [vp, i64, i64, vp, i64, i64, i32, i64, i32, i32, i32, vp, f64, vp, i64, i32, vp, i32,
+                                     vp, vp, vp, vp, i64, i32, i32, vp, i64, i32, vp, vp, vp]),
+        "slh_attend_paged_e4m3_workspace": (i64, [i32, i32, i32, i32, i32, i64, i64]),
+        "slh_attend_paged_e4m3": (i32, [vp, i64, i64, vp, vp, vp, vp, i32, i64, i32, i32, i32, i32, i32, i32, i32, vp, i64, i32,
+                                        vp, vp, i64, f64, vp, i64, i64, vp, vp, i64, vp]),
+        "slh_attend_weights_workspace": (i64, [i64, i32, i32, i32, i32, i64]),
+        "slh_attend_weights": (i32, [vp, i64, i64, vp, vp, i32, i64, i32, i32, i64, i32, i32, i32, i32, vp, i64, i32, vp, vp,
+                                     vp, f64, vp, vp, i64, vp]),
+        "slh_kv_evict_workspace": (i64, [i32, i32]),
+        "slh_kv_evict": (i32, [vp, vp, vp, vp, i32, i64, i32, i32, i32, i32, i32, vp, i64, i32, vp, vp, vp, vp, i32, i32, i32,
+                               vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
