@@ -47,8 +47,8 @@ def weights(q, k, lse, limit, scale):
     """w [Hkv, m] of rows q [n, Hq, d] over k [m, Hkv, d], lse [n, Hq]; row i sees the first limit[i] keys; and its tolerance.
 
     A weight is exp(x), x = scale s - lse: errors of s are those of d fp32 additions of products, 2 d 2^-24 scale sum |q| |k|;
-    the rounding of scale, of x and of x log2(e) (by its constant and by the product), 2^-24 each, relative to the scaled score
-    and to x; the exponential 2^-23; a sum over n terms n 2^-24."""
+    formed as 2^(s c - l) with c = scale log2(e) and l = lse log2(e) rounded, each by its constant's and its product's
+    rounding, 2 2^-24 of |scale s| and of |lse|, and one more of x; the exponential 2^-23; a sum over n terms n 2^-24."""
     n, Hq, d = q.shape
     m, Hkv = k.shape[:2]
     g = Hq // Hkv
@@ -63,7 +63,7 @@ def weights(q, k, lse, limit, scale):
             s = kk @ qq * scale
             x = s - float(lse[i, h])
             p = torch.exp(x)
-            e = 2 * d * u * (kk.abs() @ qq.abs()) * scale + u * s.abs() + 4 * u * x.abs() + 4 * u
+            e = 2 * d * u * (kk.abs() @ qq.abs()) * scale + 2 * u * (s.abs() + abs(float(lse[i, h]))) + 4 * u * x.abs() + 4 * u
             w[h // g, :c] += p
             tol[h // g, :c] += p * (e + n * g * u)
     return w, tol
