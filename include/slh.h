@@ -52,6 +52,7 @@ typedef struct slh_ctx slh_ctx;
 #define SLH_BF16 0        /* bfloat16, raw 16-bit patterns                          */
 #define SLH_F32  1        /* float32                                                */
 #define SLH_F16  2        /* float16, raw patterns: the attention operators only    */
+#define SLH_E4M3 3        /* codes with a power of two a block: slh_kv_evict only   */
 
 /* options for slh_set_option (set before slh_feature_map) */
 #define SLH_OPT_KERNEL        1  /* 0: unbiased for exp(x.y/sqrt(D)) (default): the
@@ -654,14 +655,14 @@ int slh_attend_weights(const void *q, int64_t q_st, int64_t q_sh, const void *k_
  * in its order to the first rows of the sequence's pages; rows behind are as they were.  kept[b][h][i] (device, [B][H][budget])
  * says which row became row i, -1 where there is none.  weights_out: the weights of the rows as they are now, 0 behind
  * the last.  lens_out[b] = min(lens[b], budget).  weights_out may be weights, lens_out lens.
- * Caches of dtype (SLH_BF16, SLH_F16, SLH_F32; any d of slh_kv_append, page_size a power of two up to 65536), or, with k_scale and
- * v_scale, in 8 bits (dtype is not looked at): the blocks of a sequence that is cut get the smallest power
- * of two for the rows they now hold (at least 2^-126), the codes follow, exactly but for those that become subnormal.
+ * Caches of dtype SLH_BF16, SLH_F16 or SLH_F32 (any d of slh_kv_append, page_size a power of two up to 65536; no scales), or
+ * SLH_E4M3, in 8 bits: the blocks of a sequence that is cut get the smallest power of two for the rows they now
+ * hold (at least 2^-126), the codes follow, exactly but for those that become subnormal.
  * Rows of pages outside [0, n_pages) are not read or written.  budget >= 1; first + last <= budget;
- * B H <= 2^23; max_pages page_size < 2^29.  workspace: slh_kv_evict_workspace() bytes (aligned to 16), which no other call
- * may use until this one has run.
+ * max_pages page_size < 2^29; 2 B H ceil(budget / 256) ceil(bytes of a row / 128) <= 2^22.  workspace: slh_kv_evict_workspace()
+ * bytes (aligned to 16, contents need no preparation), which no other call may use until this one has run.
  */
-int64_t slh_kv_evict_workspace(int32_t B, int32_t H);
+int64_t slh_kv_evict_workspace(int32_t B, int32_t H, int32_t d, int32_t dtype, int32_t budget);
 int slh_kv_evict(void *k_cache, void *v_cache, void *k_scale, void *v_scale, int32_t dtype,
                  int64_t n_pages, int32_t page_size, int32_t block, int32_t B, int32_t H, int32_t d,
                  const int32_t *page_table, int64_t ld_pages, int32_t max_pages,

@@ -170,9 +170,9 @@ def slh_attend_weights(q, k_cache, page_table, lens, lse, weights, cu_q=None, k_
     return weights
 
 
-def slh_kv_evict_workspace(B_, H):
-    """Bytes that slh_kv_evict needs as workspace."""
-    return int(B.load().slh_kv_evict_workspace(B_, H))
+def slh_kv_evict_workspace(B_, H, d, dtype, budget):
+    """Bytes that slh_kv_evict needs as workspace, for caches of the torch type `dtype`."""
+    return int(B.load().slh_kv_evict_workspace(B_, H, d, B.SLH_E4M3 if dtype is _CODE else _DTYPES[dtype], budget))
 
 
 def slh_kv_evict(k_cache, v_cache, weights, page_table, lens, budget, first=0, last=0, k_scale=None, v_scale=None, weights_out=None,
@@ -190,7 +190,7 @@ def slh_kv_evict(k_cache, v_cache, weights, page_table, lens, budget, first=0, l
     ln, n = _lens(lens, dev)
     if k_scale is not None or v_scale is not None:
         held, cache, block = _held(k_cache, v_cache, k_scale, v_scale, dev)
-        code = B.SLH_BF16
+        code = B.SLH_E4M3
     else:
         if dtype not in _DTYPES:
             raise SLHError(f"k_cache: unsupported type {dtype}")
@@ -210,7 +210,9 @@ def slh_kv_evict(k_cache, v_cache, weights, page_table, lens, budget, first=0, l
     wo = _plain("weights_out", weights_out, torch.float32, dev, shape)
     lo = _plain("lens_out", lens_out, torch.int32, dev, (n,))
     kp = _plain("kept", kept, torch.int32, dev, (n, H, budget))
-    need = _bytes("slh_kv_evict_workspace", dev, (n, H))
+    need = int(B.load().slh_kv_evict_workspace(n, H, d, code, budget))
+    if need < 0:
+        raise SLHError("slh_kv_evict: a size that the library does not take")
     workspace, ws = _workspace(need, dev, workspace, k_cache.device, stream)
     _call("slh_kv_evict", dev, stream,
           (*held, code, total, page, block, n, H, d, pages, ld, most, ln, lo, w, wo, budget, first, last, kp, ws, need))

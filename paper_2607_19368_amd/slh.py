@@ -15,7 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libslh.so")
 
 SLH_OK, SLH_EINVAL, SLH_ENOMEM, SLH_EHIP, SLH_ESTATE = 0, -1, -2, -3, -4
-SLH_BF16, SLH_F32, SLH_F16 = 0, 1, 2
+SLH_BF16, SLH_F32, SLH_F16, SLH_E4M3 = 0, 1, 2, 3
 SLH_ROPE_PLAIN, SLH_ROPE_LINEAR, SLH_ROPE_BASE, SLH_ROPE_BANDS = 0, 1, 2, 3
 SLH_OPT_KERNEL, SLH_OPT_WINDOW_LEN, SLH_OPT_POS_MODE, SLH_OPT_BREAKDOWN_TOL, SLH_OPT_TIMING = 1, 2, 3, 4, 5
 SLH_OPT_SHORT_WINDOWS, SLH_OPT_NORMALIZE, SLH_OPT_POS_SCHEME, SLH_OPT_KEEP_LAST = 6, 7, 8, 9
@@ -103,7 +103,7 @@ def load():
         "slh_attend_weights_workspace": (i64, [i64, i32, i32, i32, i32, i64]),
         "slh_attend_weights": (i32, [vp, i64, i64, vp, vp, i32, i64, i32, i32, i64, i32, i32, i32, i32, vp, i64, i32, vp, vp,
                                      vp, f64, vp, vp, i64, vp]),
-        "slh_kv_evict_workspace": (i64, [i32, i32]),
+        "slh_kv_evict_workspace": (i64, [i32, i32, i32, i32, i32]),
         "slh_kv_evict": (i32, [vp, vp, vp, vp, i32, i64, i32, i32, i32, i32, i32, vp, i64, i32, vp, vp, vp, vp, i32, i32, i32,
                                vp, vp, i64, vp]),
     }

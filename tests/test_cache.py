@@ -482,7 +482,7 @@ def test_evict_budgets(budget, first, last):
 
 
 @pytest.mark.parametrize("block", [0, 64])
-@pytest.mark.parametrize("n,budget", [(1024, 1023), (1025, 512), (3000, 700), (5003, 1)])
+@pytest.mark.parametrize("n,budget", [(1024, 1023), (1025, 512), (3000, 700), (5003, 1), (25000, 3001), (24576, 24575), (60011, 1300)])
 def test_evict_long(n, budget, block):
     """Chunks of the pass over the weights and of the move, and their ends."""
     _evict_case([n, 17], budget, 0, 0, 2, 64, BF, 64, block, n)
