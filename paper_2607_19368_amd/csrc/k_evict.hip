@@ -47,13 +47,11 @@ __device__ __forceinline__ uint32_t ev_key(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-
-
 // and back
 __device__ __forceinline__ float ev_weight(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
 constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64;
-constexpr int EV_BINS = 4096, EV_LIST = 2048;
+constexpr int EV_BINS = 4096, EV_LIST = 1024;
 
 constexpr int EM_THREADS = 512, EM_PASS = EM_THREADS / 8, EM_N = 4, EM_ROWS = EM_PASS * EM_N;   // 8 lanes a row
 static_assert(EM_ROWS >= C8_BLOCK_MOST, "a chunk holds whole blocks");
@@ -85,8 +83,6 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   // rows of this wave, 64 at a time
   const int steps = (n + EV_THREADS - 1) / EV_THREADS, in_lds = min(steps, LDS), row0 = wave * steps * 64 + lane;
   auto key_of = [&](int i) { return row0 + 64 * i < n ? ev_key(w[row0 + 64 * i]) : 0u; };
-#pragma unroll 8
-  for (int i = 0; i < in_lds; ++i) s_key[i * EV_THREADS + tid] = key_of(i);
   auto each = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll 4
     for (int i = 0; i < in_lds; ++i) f(row0 + 64 * i, s_key[i * EV_THREADS + tid]);
@@ -96,6 +92,7 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   // candidates: rows [lo, lo + m), of which `need` stay
   const int lo = a.first, m = n - a.last - lo;
   int need = a.budget - a.first - a.last;
+  auto is_candidate = [&](int j) { return (unsigned)(j - lo) < (unsigned)m; };
   auto clear = [&] {
     for (int i = tid; i < EV_BINS; i += EV_THREADS) s_hist[i] = 0;
     __syncthreads();
@@ -122,33 +119,56 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
     need = s_found[1];
     return (uint32_t)s_found[0];
   };
-  uint32_t least = 0xffffffffu;                    // the smallest weight that stays; none: behind all of them
+  // rows that stay for sure, and those with the smallest weight that stays, of which the first `need` do
+  uint32_t least = 0xffffffffu;                    // none: behind all of them
+  auto kind = [&](int j, uint32_t k, unsigned long long& same, unsigned long long& sure) __attribute__((always_inline)) {
+    const bool candidate = is_candidate(j);
+    same = __ballot(candidate && k == least);
+    sure = __ballot(candidate ? k > least : j < n);
+  };
+  clear();
+  auto take = [&](int i, uint32_t k) __attribute__((always_inline)) {
+    if (i < LDS) s_key[i * EV_THREADS + tid] = k;
+    if (is_candidate(row0 + 64 * i)) atomicAdd(&s_hist[k >> 20], 1);
+  };
+  for (int i0 = 0; i0 < steps; i0 += 8) {
+    uint32_t k[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) k[e] = i0 + e < steps ? key_of(i0 + e) : 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (i0 + e < steps) take(i0 + e, k[e]);
+  }
+  int n_same = 0, n_sure = 0;                      // of this wave
+  bool short_list = false;
   if (need > 0) {
-    clear();
-    each([&](int j, uint32_t k) {
-      if ((unsigned)(j - lo) < (unsigned)m) atomicAdd(&s_hist[k >> 20], 1);
-    });
     const uint32_t top = find();
-    // those that share the upper bits: into a list in the place of the counts' upper half, or, where they are too many,
-    // all rows are gone through again
+    // those that share the upper bits: into a list in the place of the counts' upper half, key and wave, or, where they are
+    // too many, all rows are gone through again
     if (tid == 0) s_listed = 0;
     __syncthreads();
-    uint32_t* const listed = (uint32_t*)s_hist + EV_BINS - EV_LIST;
+    uint32_t* const listed = (uint32_t*)s_hist + EV_BINS - 2 * EV_LIST;
     each([&](int j, uint32_t k) {
-      const bool in = (unsigned)(j - lo) < (unsigned)m && k >> 20 == top;
+      const bool candidate = is_candidate(j), in = candidate && k >> 20 == top;
+      n_sure += __popcll(__ballot(candidate ? k >> 20 > top : j < n));
       const unsigned long long who = __ballot(in);
       if (!who) return;
       int to = 0;
       if (lane == 0) to = atomicAdd(&s_listed, __popcll(who));
       to = __builtin_amdgcn_readfirstlane(to) + __popcll(who & ((1ull << lane) - 1));
-      if (in && to < EV_LIST) listed[to] = k;
+      if (in && to < EV_LIST) listed[to] = k, listed[EV_LIST + to] = wave;
     });
+    if (lane == 0) s_sure[wave] = n_sure;
     __syncthreads();
     const int many = s_listed;
-    const bool short_list = many <= EV_LIST;
-    uint32_t mine[EV_LIST / EV_THREADS];
+    short_list = many <= EV_LIST;
+    uint32_t mine[EV_LIST / EV_THREADS], of[EV_LIST / EV_THREADS];
 #pragma unroll
-    for (int e = 0; e < EV_LIST / EV_THREADS; ++e) mine[e] = short_list && tid + e * EV_THREADS < many ? listed[tid + e * EV_THREADS] : 0;
+    for (int e = 0; e < EV_LIST / EV_THREADS; ++e) {
+      const bool there = short_list && tid + e * EV_THREADS < many;
+      mine[e] = there ? listed[tid + e * EV_THREADS] : 0;
+      of[e] = there ? listed[EV_LIST + tid + e * EV_THREADS] : 0;
+    }
     __syncthreads();
     uint32_t prefix = top << 20;
 #pragma unroll 1
@@ -161,35 +181,39 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
           if (tid + e * EV_THREADS < many && (mine[e] & above) == prefix) atomicAdd(&s_hist[mine[e] >> shift & 1023], 1);
       } else {
         each([&](int j, uint32_t k) {
-          if ((unsigned)(j - lo) < (unsigned)m && (k & above) == prefix) atomicAdd(&s_hist[k >> shift & 1023], 1);
+          if (is_candidate(j) && (k & above) == prefix) atomicAdd(&s_hist[k >> shift & 1023], 1);
         });
       }
       prefix |= find() << shift;
     }
     least = prefix;
+    __syncthreads();
+    if (short_list) {                              // of the list, by the waves whose rows they are
+      if (tid < EV_WAVES) s_same[tid] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < EV_LIST / EV_THREADS; ++e)
+        if (tid + e * EV_THREADS < many && mine[e] >= least) atomicAdd(mine[e] > least ? &s_sure[of[e]] : &s_same[of[e]], 1);
+    }
   }
-  // rows above it, and the first `need` of those equal to it
-  int n_same = 0, n_sure = 0;
-  auto kind = [&](int j, uint32_t k, unsigned long long& same, unsigned long long& sure) __attribute__((always_inline)) {
-    const bool candidate = (unsigned)(j - lo) < (unsigned)m;
-    same = __ballot(candidate && k == least);
-    sure = __ballot(candidate ? k > least : j < n);
-  };
-  each([&](int j, uint32_t k) {
-    unsigned long long same, sure;
-    kind(j, k, same, sure);
-    n_same += __popcll(same), n_sure += __popcll(sure);
-  });
-  __syncthreads();
-  if (lane == 0) s_same[wave] = n_same, s_sure[wave] = n_sure;
+  if (!short_list) {
+    n_sure = 0;
+    each([&](int j, uint32_t k) {
+      unsigned long long same, sure;
+      kind(j, k, same, sure);
+      n_same += __popcll(same), n_sure += __popcll(sure);
+    });
+    __syncthreads();
+    if (lane == 0) s_same[wave] = n_same, s_sure[wave] = n_sure;
+  }
   __syncthreads();
   int equal = 0, done = 0;
 #pragma unroll
   for (int v = 0; v < EV_WAVES; ++v)
     if (v < wave) equal += s_same[v], done += s_sure[v];
-  // weights_out may be the weights: where all are held, they are written as they are listed; else rows are listed first,
-  // and their weights moved a chunk at a time, a chunk's loads before its stores
-  const bool all_held = steps <= LDS;
+  // weights_out may be the weights: where not all are held, rows are listed first then, and their weights moved a chunk at a
+  // time, a chunk's loads before its stores
+  const bool all_held = steps <= LDS || a.w != a.w_out;
   each([&](int j, uint32_t k) {
     unsigned long long same, sure;
     kind(j, k, same, sure);
