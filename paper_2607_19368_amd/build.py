@@ -39,6 +39,7 @@ SOURCES = [
     "attend_api.cpp",
     "k_append8.hip",
     "k_rows8.hip",
+    "k_tiles8.hip",
     "attend8_api.cpp",
     "k_weights.hip",
     "k_evict.hip",

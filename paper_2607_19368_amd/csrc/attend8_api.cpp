@@ -5,8 +5,9 @@
 namespace slh {
 
 // As ATTEND_COSTS, for the kernels of 8-bit keys.
-static const AttendCost ATTEND8_COSTS[2] = {{16, 1.8, 0.65, 0.8, 0.33}, {32, 2.5, 0.75, 0.95, 0.42}};
-static const AttendKind ATTEND_8 = {ATTEND8_COSTS, 2, 1.0};
+static const AttendCost ATTEND8_COSTS[3] = {
+    {16, 1.8, 0.65, 0.8, 0.33}, {32, 2.5, 0.75, 0.95, 0.42}, {AT_ROWS, 3.0, 1.13, 1.75, 0.95}};
+static const AttendKind ATTEND_8 = {ATTEND8_COSTS, 3, 1.0};
 
 static bool attend8_sizes_ok(int B, int n_q, int Hq, int Hkv, int d, int64_t max_len, int64_t prefix_len) {
   return attend_common_ok(SLH_BF16, B, Hq, Hkv, d, 1.0) && attend_paged_ok(B, n_q, Hq / Hkv, max_len, prefix_len);
@@ -44,7 +45,7 @@ int slh_attend_paged_e4m3(const void* q, int64_t q_st, int64_t q_sh, const void*
   AttendArgs& a = x.a;
   a.q = (const uint16_t*)q, a.q_st = q_st, a.q_sh = q_sh;
   a.k = (const uint16_t*)k_cache, a.v = (const uint16_t*)v_cache;
-  x.k_two = (const uint8_t*)k_scale, x.v_two = (const uint8_t*)v_scale, x.lg_block = __builtin_ctz((unsigned)block);
+  x.held = AtHeld{(const uint8_t*)k_scale, (const uint8_t*)v_scale, __builtin_ctz((unsigned)block)};
   a.out = (uint16_t*)out, a.o_st = o_st, a.o_sh = o_sh, a.lse = lse;
   a.Hq = Hq, a.Hkv = Hkv, a.g = g, a.c = (float)(scale * 1.4426950408889634), a.scale = (float)scale, a.B = B, a.causal = 1;
   a.pages = page_table, a.ld_pages = ld_pages, a.max_pages = max_pages, a.lens = lens;
@@ -69,14 +70,19 @@ int slh_attend_paged_e4m3(const void* q, int64_t q_st, int64_t q_sh, const void*
   const bool bf16 = dtype == SLH_BF16;
   hipStream_t s = (hipStream_t)stream;
   (void)hipGetLastError();
+  auto go = [&](int rows, int64_t blocks) {
+    return rows == AT_ROWS ? launch_tiles8(x, bf16, d, blocks, s) : launch_rows8(x, bf16, rows, d, blocks, s);
+  };
   hipError_t e;
-  if (pre && p.pre.rows != p.own.rows) {
-    e = launch_rows8(x, bf16, p.pre.rows, d, pre, s);
+  if (pre && p.pre.rows == AT_ROWS && p.own.rows != AT_ROWS) {
+    e = launch_both8(x, bf16, p.own.rows, d, pre, pre + own, s);
+  } else if (pre && p.pre.rows != p.own.rows) {
+    e = go(p.pre.rows, pre);
     if (e != hipSuccess) return SLH_EHIP;
     a.pre_tiles = 0;
-    e = launch_rows8(x, bf16, p.own.rows, d, own, s);
+    e = go(p.own.rows, own);
   } else {
-    e = launch_rows8(x, bf16, p.own.rows, d, pre + own, s);
+    e = go(p.own.rows, pre + own);
   }
   if (e == hipSuccess && p.bytes) e = launch_attend_join(a, bf16, d, p.slots, s);
   return e == hipSuccess ? SLH_OK : SLH_EHIP;

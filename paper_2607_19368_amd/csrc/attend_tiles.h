@@ -32,9 +32,7 @@
 // and the rest of a tile's time is its softmax.  23 causal sequences of 59 to 1458 tokens, 32 / 8 heads, 136 us = 667 TFLOP/s:
 // of a block's 23 us, 7 are its task, first loads and last stores, and 10 % of the products are masked.
 #pragma once
-#include "attend.h"
-
-#include <type_traits>
+#include "attend_held.h"
 
 namespace slh {
 
@@ -65,8 +63,10 @@ __device__ __forceinline__ void at_tile_barrier() {
 template <int D> constexpr int at_lds_tile() { return AT_KEYS * D + 64; }
 template <int D> constexpr int at_lds() { return 4 * at_lds_tile<D>() + 2 * AT_WAVES; }
 
-template <class TY, int D, bool PAGED, int KW>
-__device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uint16_t* smem) {
+// E8: keys and values of a cache in 8 bits.  They wait in registers while the tile before is worked on, and are converted to
+// TY, with their powers of two, on the way to LDS, once for the block's 128 rows.
+template <class TY, int D, bool PAGED, int KW, bool E8 = false>
+__device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uint16_t* smem, const AtHeld& held = AtHeld{}) {
   constexpr int CH = D / 8;                        // 16-byte chunks of a row
   constexpr int KS = D / 16;                       // k steps of K Q^T
   constexpr int DB = (D + 31) / 32;                // 32-row blocks of O^T
@@ -175,6 +175,51 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     }
   };
 
+  // Of a cache in 8 bits: 16 codes of row r of K and of V a load, this lane's part c of the row.
+  constexpr int CH8 = D / 16, NC8 = AT_KEYS * CH8, LD8 = E8 ? (NC8 + 64 * AT_WAVES - 1) / (64 * AT_WAVES) : 1;
+  at_u32x4 k8[LD8], v8[LD8];
+  int k8_two[LD8], v8_two[LD8], page8[LD8];
+  auto row8 = [&](int x) { return min((x * 64 * AT_WAVES + tid) / CH8, AT_KEYS - 1); };
+  auto part8 = [&](int x) { return (x * 64 * AT_WAVES + tid) % CH8; };
+  auto pages8 = [&](int tile) {
+#pragma unroll
+    for (int x = 0; x < LD8; ++x)
+      page8[x] = one_page ? ((at_const_ints)t.list)[tile >> (a.lg_page - 6)] : t.list[min(tile * AT_KEYS + row8(x), t.nk - 1) >> a.lg_page];
+  };
+  auto load8 = [&](int tile) {
+#pragma unroll
+    for (int x = 0; x < LD8; ++x) {
+      const int j = min(tile * AT_KEYS + row8(x), t.nk - 1);
+      const int64_t p = (unsigned)page8[x] < (unsigned)a.n_pages ? page8[x] : 0;
+      const int64_t line = ((p * a.Hkv + kvh) << a.lg_page) + (j & ((1 << a.lg_page) - 1));
+      k8[x] = *(const at_u32x4*)((const uint8_t*)a.k + line * D + 16 * part8(x));
+      v8[x] = *(const at_u32x4*)((const uint8_t*)a.v + line * D + 16 * part8(x));
+      k8_two[x] = held.k_two[line >> held.lg_block];
+      v8_two[x] = held.v_two[line >> held.lg_block];
+    }
+  };
+  auto put8 = [&](int buf) {
+    if constexpr (E8) {
+#pragma unroll
+      for (int x = 0; x < LD8; ++x) {
+        if (NC8 % (64 * AT_WAVES) != 0 && x * 64 * AT_WAVES + tid >= NC8) break;
+        const int r = row8(x), c = 2 * part8(x);
+        uint16_t* const kr = sK + buf * at_lds_tile<D>() + r * D;
+        uint16_t* const vr = sV + buf * at_lds_tile<D>() + r * D;
+        const float kt = c8_two(k8_two[x]), vt = c8_two(v8_two[x]);
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+          *(at_u32x4*)(kr + 8 * ((c + h2) ^ at_kswz<D>(r))) =
+              at_u32x4{c8_pair<TY, false>(k8[x][2 * h2], kt), c8_pair<TY, true>(k8[x][2 * h2], kt),
+                       c8_pair<TY, false>(k8[x][2 * h2 + 1], kt), c8_pair<TY, true>(k8[x][2 * h2 + 1], kt)};
+          *(at_u32x4*)(vr + 8 * ((c + h2) ^ at_vswz<D>(r))) =
+              at_u32x4{c8_pair<TY, false>(v8[x][2 * h2], vt), c8_pair<TY, true>(v8[x][2 * h2], vt),
+                       c8_pair<TY, false>(v8[x][2 * h2 + 1], vt), c8_pair<TY, true>(v8[x][2 * h2 + 1], vt)};
+        }
+      }
+    }
+  };
+
   at_f32x16 o[DB];
 #pragma unroll
   for (int b = 0; b < DB; ++b)
@@ -228,7 +273,9 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-    if (next >= 0 && is_even(next)) {
+    if constexpr (E8) {
+      scores(std::false_type{}, s, ck, nullptr, nullptr, nbuf);
+    } else if (next >= 0 && is_even(next)) {
       scores(std::true_type{}, s, ck, kbase + even_at(next, k_st), vbase + even_at(next, v_st), nbuf);
     } else {
       if (next >= 0) load_tile(next, nbuf);
@@ -237,7 +284,11 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     // Behind the last product stands, where the waves share a tile's loads unevenly, a short branch around one of them.
     // The branch on `masked` needs no wait of its own: its longer way, two instructions a score, is more than the 12 states, so
     // that the compiler counts the other too (a wait for every size: 128 sequences behind 32768 keys 89.7 instead of 87.9 us).
-    if constexpr (NL % AT_WAVES != 0) at_products_done(s);
+    if constexpr (NL % AT_WAVES != 0 || E8) at_products_done(s);
+    if constexpr (E8) {
+      if (next >= 0) put8(nbuf);
+      if (next >= 0 && next + 1 < t1) load8(next + 1);
+    }
     if (masked) {
       int left = limit - j0 - 32 * NB * kw - 4 * half;
       asm volatile("" : "+v"(left));               // a branch, not 32 selects in every tile
@@ -357,19 +408,35 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     __syncthreads();
   };
 
-  if (t0 < t1) {
+  if constexpr (E8) {
+    if (t0 < t1) {
+      pages8(t0);
+      load8(t0);
+      pages8(min(t0 + 1, t1 - 1));
+      put8(0);
+      if (t0 + 1 < t1) load8(t0 + 1);
+      pages8(min(t0 + 2, t1 - 1));
+    }
+  } else if (t0 < t1) {
     find_pages(t0);
     load_tile(t0, 0);
     find_pages(min(t0 + 1, t1 - 1));
   }
   for (int tile = t0; tile < t1; ++tile) {
     const int buf = (tile - t0) & 1;
-    at_tile_barrier();                             // this tile has landed; the other buffer is free
+    // this tile has landed; the other buffer is free
+    if constexpr (E8)
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else
+      at_tile_barrier();
     const int j0 = tile * AT_KEYS;
     if (block_least < j0 + AT_KEYS) clean_tile(sV + buf * at_lds_tile<D>(), j0);
     tile_step(least < j0 + AT_KEYS, sK + buf * at_lds_tile<D>(), sV + buf * at_lds_tile<D>(), j0, tile + 1 < t1 ? tile + 1 : -1,
               buf ^ 1);
-    find_pages(min(tile + 2, t1 - 1));
+    if constexpr (E8)
+      pages8(min(tile + 3, t1 - 1));
+    else
+      find_pages(min(tile + 2, t1 - 1));
   }
 
   at_products_done(o);

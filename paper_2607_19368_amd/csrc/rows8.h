@@ -81,8 +81,8 @@ __device__ __forceinline__ void rows8(const Attend8Args& A, int block, float* sm
     for (int f = 0; f < 2; ++f) {
       const int64_t p = (unsigned)page[f] < (unsigned)a.n_pages ? page[f] : 0;
       const int64_t line = ((p * a.Hkv + kvh) << a.lg_page) + (row_of(u, f) & in_page);
-      s.k_two[f] = A.k_two[line >> A.lg_block];
-      s.v_two[f] = A.v_two[line >> A.lg_block];
+      s.k_two[f] = A.held.k_two[line >> A.held.lg_block];
+      s.v_two[f] = A.held.v_two[line >> A.held.lg_block];
       const uint8_t* const kt = kbase + line * D;
       const uint8_t* const vt = vbase + line * D;
 #pragma unroll
