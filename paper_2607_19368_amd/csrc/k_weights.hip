@@ -2,11 +2,8 @@
 //   w[b][h][j] += sum over queries i and query heads of h that see key j of exp(scale q_i . k_j - lse_i)
 //
 // A key belongs to one wave, which goes through the rows ((token, query head) pairs) that see it: no atomics, the
-// same bits every run.  S (rows x keys) = Q K^T by v_mfma_f32_16x16x32, so that a lane holds four rows of one
-// key and adds within its registers; the four lane groups of a key are added at the end.
-//
-// The exponent is formed as scale s - lse, in that order, and multiplied by log2(e) after: both sides may be large, and
-// only their difference has to be exact.  Everything is fp32.
+// same bits every run.  S (rows x keys) = Q K^T, so that a lane holds several rows of one key and adds within its
+// registers; the lanes of a key are added at the end.  Everything is fp32.
 #include "attend8.h"
 #include "attend_plan.h"
 
@@ -33,11 +30,15 @@ struct WeightArgs {
   float* part;             // [runs][2][Hkv][256]
 };
 
-constexpr int WT_KEYS = 32;              // of a wave
+// ---- few rows: the new tokens of a batch ----
+// A wave takes 64 keys and holds them while it goes through the rows, 16 at a time.  Bound by reading K once: everything that
+// does not wait for the page table goes out in front of it, and the keys all at once.
+constexpr int WT_KEYS = 64;              // of a wave
 
 template <class TY, int D, bool E8>
 __global__ __launch_bounds__(256) void k_weights(WeightArgs a) {
   constexpr int KS = (D + 31) / 32, X = D / 64, R = D % 64, KT = WT_KEYS / 16;
+  constexpr int KL = E8 ? X : KS;        // 16-byte loads of a key by a lane
   const int lane = threadIdx.x & 63, r16 = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int x = blockIdx.x;
@@ -49,77 +50,107 @@ __global__ __launch_bounds__(256) void k_weights(WeightArgs a) {
   const int64_t q0 = max((int64_t)0, min(a.cu ? (int64_t)a.cu[b] : (int64_t)b * a.n_each, a.Tq));
   const int64_t q1 = max((int64_t)0, min(a.cu ? (int64_t)a.cu[b + 1] : (int64_t)(b + 1) * a.n_each, a.Tq));
   const int nq = (int)max((int64_t)0, q1 - q0), rows = nq * a.g;
+  int r0 = max(0, key0 - (n - nq)) * a.g;          // the first row that sees one of the keys
+  if (r0 >= rows) return;
 
-  // keys of this lane, one of each 16, in the type of the queries
-  at_u32x4 kf[KT][KS];
+  // this lane's key of each 16
+  int64_t line[KT];
+  int page[KT];
 #pragma unroll
-  for (int t = 0; t < KT; ++t) {
-    const int j = min(key0 + 16 * t + r16, n - 1);
-    const int page = a.pages[b * a.ld_pages + (j >> a.lg_page)];
-    const int64_t line = (((int64_t)((unsigned)page < (unsigned)a.n_pages ? page : 0) * a.Hkv + kvh) << a.lg_page) +
-                         (j & ((1 << a.lg_page) - 1));
-    if constexpr (E8) {
-      const uint8_t* kp = (const uint8_t*)a.k + line * D;
-      const float two = c8_two(a.k_two[line >> a.lg_block]);
+  for (int t = 0; t < KT; ++t) page[t] = a.pages[b * a.ld_pages + (min(key0 + 16 * t + r16, n - 1) >> a.lg_page)];
+  // and, in the first group of lanes, its sum so far
+  float* const w = a.w + ((int64_t)b * a.Hkv + kvh) * a.max_rows + key0 + r16;
+  float was[KT];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        at_u32x2 c = {0, 0};
-        if (!R || s < KS - 1)
-          c = *(const at_u32x2*)(kp + 64 * (s / 2) + 16 * grp + 8 * (s & 1));
-        else if (8 * grp < R)
-          c = *(const at_u32x2*)(kp + 64 * X + 8 * grp);
-        kf[t][s] = at_u32x4{c8_pair<TY, false>(c[0], two), c8_pair<TY, true>(c[0], two), c8_pair<TY, false>(c[1], two),
-                            c8_pair<TY, true>(c[1], two)};
-      }
-    } else {
-      const uint16_t* kp = (const uint16_t*)a.k + line * D;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        kf[t][s] = at_u32x4{0, 0, 0, 0};
-        if (32 * s + 8 * grp < D) kf[t][s] = *(const at_u32x4*)(kp + 32 * s + 8 * grp);
-      }
-    }
-  }
-  // first element of a row in step s
+  for (int t = 0; t < KT; ++t) was[t] = grp == 0 && key0 + 16 * t + r16 < n ? w[16 * t] : 0.f;
+
+  // first element of a row in step s: with codes, a lane's 16 bytes of a key are those of two steps
   auto d_of = [&](int s) {
     if (!E8) return 32 * s + 8 * grp;
     return !R || s < KS - 1 ? 64 * (s / 2) + 16 * grp + 8 * (s & 1) : 64 * X + 8 * grp;
   };
+  at_u32x4 qf[KS];
+  float lse[4];
+  int limit[4];
+  auto rows_of = [&] {
+    const int rr = min(r0 + r16, rows - 1), i = rr / a.g, h = kvh * a.g + rr - i * a.g;
+    const uint16_t* qp = a.q + (q0 + i) * a.q_st + h * a.q_sh;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      qf[s] = at_u32x4{0, 0, 0, 0};
+      if (d_of(s) < D) qf[s] = *(const at_u32x4*)(qp + d_of(s));
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = min(r0 + 4 * grp + e, rows - 1), tok = row / a.g;
+      lse[e] = a.lse[(q0 + tok) * a.Hq + kvh * a.g + row - tok * a.g];
+      limit[e] = r0 + 4 * grp + e < rows ? n - nq + tok + 1 : 0;
+    }
+  };
+  rows_of();
+
+  at_u32x4 k[KT][KL];
+  at_u32x2 kr[KT];
+  int two[KT];
+#pragma unroll
+  for (int t = 0; t < KT; ++t) {
+    const int j = min(key0 + 16 * t + r16, n - 1);
+    line[t] = (((int64_t)((unsigned)page[t] < (unsigned)a.n_pages ? page[t] : 0) * a.Hkv + kvh) << a.lg_page) +
+              (j & ((1 << a.lg_page) - 1));
+    if constexpr (E8) {
+      const uint8_t* kp = (const uint8_t*)a.k + line[t] * D;
+#pragma unroll
+      for (int s = 0; s < KL; ++s) k[t][s] = *(const at_u32x4*)(kp + 64 * s + 16 * grp);
+      kr[t] = at_u32x2{0, 0};
+      if (R && 8 * grp < R) kr[t] = *(const at_u32x2*)(kp + 64 * X + 8 * grp);
+      two[t] = a.k_two[line[t] >> a.lg_block];
+    } else {
+      const uint16_t* kp = (const uint16_t*)a.k + line[t] * D;
+#pragma unroll
+      for (int s = 0; s < KL; ++s) {
+        k[t][s] = at_u32x4{0, 0, 0, 0};
+        if (32 * s + 8 * grp < D) k[t][s] = *(const at_u32x4*)(kp + 32 * s + 8 * grp);
+      }
+    }
+  }
 
   float sum[KT];
 #pragma unroll
   for (int t = 0; t < KT; ++t) sum[t] = 0.f;
-  // the first row that sees one of the keys
-  for (int r0 = max(0, key0 - (n - nq)) * a.g; r0 < rows; r0 += 16) {
-    const int rr = min(r0 + r16, rows - 1), i = rr / a.g, h = kvh * a.g + rr - i * a.g;
-    const uint16_t* qp = a.q + (q0 + i) * a.q_st + h * a.q_sh;
-    at_f32x4 sc[KT];
+  const float c = a.scale * 1.44269504f;
+  auto work = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < KT; ++t) sc[t] = at_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < KT; ++t) {
+      at_f32x4 sc[1] = {at_f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      at_u32x4 qf = {0, 0, 0, 0};
-      if (d_of(s) < D) qf = *(const at_u32x4*)(qp + d_of(s));
-#pragma unroll
-      for (int t = 0; t < KT; ++t) sc[t] = TY::mfma16(qf, kf[t][s], sc[t]);
-    }
-    at_products_done(sc);
-    float part[KT];
-#pragma unroll
-    for (int t = 0; t < KT; ++t) part[t] = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int row = r0 + 4 * grp + e, tok = row / a.g;
-      const float lse = row < rows ? a.lse[(q0 + tok) * a.Hq + kvh * a.g + row - tok * a.g] : -INFINITY;
-      const int limit = lse == -INFINITY ? 0 : n - nq + tok + 1;         // such a row has no weights to give
-#pragma unroll
-      for (int t = 0; t < KT; ++t) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][e], a.scale, -lse) * 1.44269504f);
-        part[t] += key0 + 16 * t + r16 < limit ? p : 0.f;
+      for (int s = 0; s < KS; ++s) {
+        at_u32x4 kf;
+        if constexpr (E8) {
+          const bool rest = R && s == KS - 1;
+          const uint32_t c0 = rest ? kr[t][0] : k[t][s / 2 < KL ? s / 2 : 0][2 * (s & 1)];
+          const uint32_t c1 = rest ? kr[t][1] : k[t][s / 2 < KL ? s / 2 : 0][2 * (s & 1) + 1];
+          const float by = c8_two(two[t]);
+          kf = at_u32x4{c8_pair<TY, false>(c0, by), c8_pair<TY, true>(c0, by), c8_pair<TY, false>(c1, by), c8_pair<TY, true>(c1, by)};
+        } else {
+          kf = k[t][s];
+        }
+        sc[0] = TY::mfma16(qf[s], kf, sc[0]);
       }
-    }
+      at_products_done(sc);
+      float part = 0.f;
 #pragma unroll
-    for (int t = 0; t < KT; ++t) sum[t] += part[t];
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[0][e], c, -lse[e] * 1.44269504f));
+        // a row without an lse has no weights to give
+        part += key0 + 16 * t + r16 < limit[e] && lse[e] != -INFINITY ? p : 0.f;
+      }
+      sum[t] += part;
+    }
+  };
+  work();
+  while ((r0 += 16) < rows) {
+    rows_of();
+    work();
   }
 #pragma unroll
   for (int t = 0; t < KT; ++t) {
@@ -127,8 +158,7 @@ __global__ __launch_bounds__(256) void k_weights(WeightArgs a) {
     sum[t] = __uint_as_float(w32[0]) + __uint_as_float(w32[1]);
     const auto w16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum[t]), __float_as_uint(sum[t]), false, false);
     sum[t] = __uint_as_float(w16[0]) + __uint_as_float(w16[1]);
-    const int j = key0 + 16 * t + r16;
-    if (grp == 0 && j < n) a.w[((int64_t)b * a.Hkv + kvh) * a.max_rows + j] += sum[t];
+    if (grp == 0 && key0 + 16 * t + r16 < n) w[16 * t] = was[t] + sum[t];
   }
 }
 

@@ -277,29 +277,25 @@ __device__ __forceinline__ void rows8(const Attend8Args& A, int block, float* sm
     }
   };
 
+  // The next step's loads go out in front of a step's work, at the end of the keys the last step's again: a branch around
+  // them would leave the compiler to wait for as many loads as the shorter way has in flight.
   Step s0, s1;
   const int first = __builtin_amdgcn_readfirstlane(u0 + wave);
   int page[2] = {0, 0};
+  auto pages_of = [&](int u) { page[0] = page_of(min(u, u1 - 1), 0), page[1] = page_of(min(u, u1 - 1), 1); };
   if (first < u1) {
-    page[0] = page_of(first, 0), page[1] = page_of(first, 1);
+    pages_of(first);
     load(first, page, s0);
-    const int next = min(first + AT_WAVES, u1 - 1);
-    page[0] = page_of(next, 0), page[1] = page_of(next, 1);
+    pages_of(first + AT_WAVES);
   }
   for (int u = first; u < u1; u += 2 * AT_WAVES) {
-    const int n1 = u + AT_WAVES, n2 = u + 2 * AT_WAVES, n3 = u + 3 * AT_WAVES;
-    if (n1 < u1) {
-      load(n1, page, s1);
-      const int c = min(n2, u1 - 1);
-      page[0] = page_of(c, 0), page[1] = page_of(c, 1);
-    }
+    const int n1 = u + AT_WAVES, n2 = u + 2 * AT_WAVES;
+    load(min(n1, u1 - 1), page, s1);
+    pages_of(n2);
     step(u, s0);
     if (n1 >= u1) break;
-    if (n2 < u1) {
-      load(n2, page, s0);
-      const int c = min(n3, u1 - 1);
-      page[0] = page_of(c, 0), page[1] = page_of(c, 1);
-    }
+    load(min(n2, u1 - 1), page, s0);
+    pages_of(n2 + AT_WAVES);
     step(n1, s1);
   }
 
