@@ -54,15 +54,13 @@ __global__ __launch_bounds__(WPU < 4 ? 256 : 64 * WPU) void k_append8(Append8Arg
   int b = 0, begin = 0, end = 0, row0 = 0, tok_end = 0;
   if (unit < a.units) {
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-      int lo = 0, hi = 0, t1 = 0, n = 0;
-      if (b0 + lane < a.B) {
-        const int64_t q0 = a.cu ? a.cu[b0 + lane] : (int64_t)(b0 + lane) * a.n_each;
-        const int64_t q1 = a.cu ? a.cu[b0 + lane + 1] : q0 + a.n_each;
-        t1 = (int)max((int64_t)0, min(q1, a.T));
-        n = max(0, t1 - (int)max((int64_t)0, min(q0, a.T)));
-        hi = min(max(a.lens[b0 + lane], 0), most);
-        lo = max(0, hi - n);
-      }
+      // lanes past the last sequence read its entries and have no blocks; loads under a branch would wait in it, one by one
+      const int s = min(b0 + lane, a.B - 1);
+      const int* const cu = a.cu ? a.cu + s : a.lens;
+      const int c0 = cu[0], c1 = cu[a.cu ? 1 : 0], len = a.lens[s];
+      const int64_t q0 = a.cu ? (int64_t)c0 : (int64_t)s * a.n_each, q1 = a.cu ? (int64_t)c1 : q0 + a.n_each;
+      const int t1 = (int)max((int64_t)0, min(q1, a.T)), n = max(0, t1 - (int)max((int64_t)0, min(q0, a.T)));
+      const int hi = b0 + lane < a.B ? min(max(len, 0), most) : 0, lo = max(0, hi - n);
       const int count = hi > lo ? ((hi - 1) >> a.lg_block) - (lo >> a.lg_block) + 1 : 0;
       const int upto = c8_wave_scan(count);
       const unsigned long long hit = __ballot(upto > at);
@@ -79,33 +77,51 @@ __global__ __launch_bounds__(WPU < 4 ? 256 : 64 * WPU) void k_append8(Append8Arg
       at -= __builtin_amdgcn_readlane(upto, 63);
     }
   }
-  int64_t line = 0;                                             // of the block's first row, in rows of the cache
-  if (real) {
-    const int page = a.pages[b * a.ld_pages + (row0 >> a.lg_page)];
-    real = (unsigned)page < (unsigned)a.n_pages;
-    if (real) line = (((int64_t)page * a.H + h) << a.lg_page) + (row0 & ((1 << a.lg_page) - 1));
-  }
-  uint8_t* const cache = a.cache[kv] + line * a.form.d;
-  uint8_t* const two = a.two[kv] + (line >> a.lg_block);
-  const int before = real ? max(0, begin - row0) : 0;           // earlier rows of the sequence in the block
-  if (WPU > 1 && strip == 0 && lane == 0) s_old[mine] = before ? *two : 0;
+  // earlier rows of the sequence in the block; the rows themselves are on their way before the page is known
+  const int before = real ? max(0, begin - row0) : 0;
+  const int page = real ? a.pages[b * a.ld_pages + (row0 >> a.lg_page)] : -1;
 
+  // Every load of the rows goes out before any is looked at: where a lane has nothing to load, it loads the first token's
+  // or the first chunk.
   const int p = lane % LPR;
   const RopeLane l = rp_lane(p, kv ? 0 : a.form.rot, a.form.d);
+  const int c0 = l.has0 ? 8 * l.c0 : 0, c1 = l.has1 ? 8 * l.c1 : 0;
+  RpRaw<DT> raw[IT][2], raw_w[2];
+  int at_pos[IT];
+  bool is_new[IT];
+  const bool turn = !kv && a.form.table, norm = !kv && a.w;
+#pragma unroll
+  for (int i = 0; i < IT; ++i) {
+    const int r = 16 * strip + i * RPI + lane / LPR;
+    is_new[i] = real && r >= before && row0 + r < end;
+    const int64_t t = is_new[i] ? (int64_t)tok_end - end + row0 + r : 0;
+    const elem* src = (const elem*)a.x[kv] + t * a.st[kv] + h * a.sh[kv];
+    raw[i][0].load(src + c0), raw[i][1].load(src + c1);
+    at_pos[i] = turn ? a.pos[t] : 0;
+  }
+  if (norm) raw_w[0].load((const elem*)a.w + c0), raw_w[1].load((const elem*)a.w + c1);
+  RopeTurn turns[IT];
+  if (turn) {
+    const RopeLane first = rp_lane(0, a.form.rot, a.form.d);
+#pragma unroll
+    for (int i = 0; i < IT; ++i) turns[i] = rp_turn_of(a.form, l.pair ? l : first, l.pair ? p : 0, at_pos[i]);
+  }
   float x0[IT][8], x1[IT][8];
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < IT; ++i) {
-    const int r = 16 * strip + i * RPI + lane / LPR;
-    const bool is_new = real && r >= before && row0 + r < end;
-    const int64_t t = is_new ? (int64_t)tok_end - end + row0 + r : 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x0[i][e] = x1[i][e] = 0.f;
-    const elem* src = (const elem*)a.x[kv] + t * a.st[kv] + h * a.sh[kv];
-    if (is_new && l.has0) rp_load8<DT>(src + 8 * l.c0, x0[i]);
-    if (is_new && l.has1) rp_load8<DT>(src + 8 * l.c1, x1[i]);
-    if (!kv) rp_norm_turn<DT, LPR>(a.form, l, p, a.w, a.form.table != nullptr, a.pos + t, x0[i], x1[i]);
-    if (is_new) {
+    for (int e = 0; e < 8; ++e) {
+      x0[i][e] = is_new[i] && l.has0 ? raw[i][0].get(e) : 0.f;
+      x1[i][e] = is_new[i] && l.has1 ? raw[i][1].get(e) : 0.f;
+    }
+    if (norm) {
+      const float inv = rp_inverse<LPR>(a.form, x0[i], x1[i]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x0[i][e] = x0[i][e] * inv * raw_w[0].get(e), x1[i][e] = x1[i][e] * inv * raw_w[1].get(e);
+    }
+    if (turn && l.pair) rp_turn(a.form, turns[i], x0[i], x1[i]);
+    if (is_new[i]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t m0 = __float_as_uint(x0[i][e]) & 0x7fffffffu, m1 = __float_as_uint(x1[i][e]) & 0x7fffffffu;
@@ -115,15 +131,22 @@ __global__ __launch_bounds__(WPU < 4 ? 256 : 64 * WPU) void k_append8(Append8Arg
     }
   }
   top = c8_wave_max(top);
+  real = (unsigned)page < (unsigned)a.n_pages;
+  // of the block's first row, in rows of the cache
+  const int64_t line = real ? (((int64_t)page * a.H + h) << a.lg_page) + (row0 & ((1 << a.lg_page) - 1)) : 0;
+  uint8_t* const cache = a.cache[kv] + line * a.form.d;
+  uint8_t* const two = a.two[kv] + (line >> a.lg_block);
   int old;
   if constexpr (WPU > 1) {
     if (lane == 0) s_top[wave] = top;
+    // one wave reads the power that it will write
+    if (strip == 0 && lane == 0) s_old[mine] = real && before ? *two : 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < WPU; ++w) top = max(top, s_top[mine * WPU + w]);
     old = s_old[mine];
   } else {
-    old = before ? *two : 0;
+    old = real && before ? *two : 0;
   }
   if (!real) return;
   old = min(old, 254);

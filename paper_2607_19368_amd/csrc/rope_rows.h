@@ -48,6 +48,18 @@ __device__ __forceinline__ void rp_store8(typename RpType<DT>::elem* p, const fl
   }
 }
 
+// Eight elements as they are loaded.
+template <int DT> struct RpRaw {
+  typename RpType<DT>::vec v;
+  __device__ __forceinline__ void load(const typename RpType<DT>::elem* p) { v = *(const typename RpType<DT>::vec*)p; }
+  __device__ __forceinline__ float get(int e) const { return (float)v[e]; }
+};
+template <> struct RpRaw<SLH_F32> {
+  rp_f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *(const rp_f32x4*)p, b = *(const rp_f32x4*)(p + 4); }
+  __device__ __forceinline__ float get(int e) const { return e < 4 ? a[e] : b[e - 4]; }
+};
+
 // sum over aligned groups of LPR lanes (every lane active; the same bits in all of them)
 template <int LPR>
 __device__ __forceinline__ float rp_group_sum(float v) {
@@ -79,6 +91,55 @@ struct RopeForm {
   int64_t n_pos;
 };
 
+// The table's cosines and sines for a lane's chunks at position `at`.
+struct RopeTurn {
+  rp_f32x4 c[2], s[2];
+  float bad;              // NaN for a position that the table lacks, which shows
+};
+__device__ __forceinline__ RopeTurn rp_turn_of(const RopeForm& a, const RopeLane& l, int p, int at) {
+  const int half = a.rot >> 1;
+  const bool known = at >= 0 && at < a.n_pos;
+  const float* row_cos = a.table + (known ? (int64_t)at * a.rot : 0);
+  RopeTurn r;
+  r.bad = known ? 0.f : __builtin_nanf("");
+  // pairs (i, i + rot / 2): eights of both; pairs (2 i, 2 i + 1): four of each chunk
+  const int i0 = a.interleaved ? 4 * l.c0 : 8 * p, i1 = a.interleaved ? 4 * l.c1 : 8 * p + 4;
+  r.c[0] = *(const rp_f32x4*)(row_cos + i0), r.c[1] = *(const rp_f32x4*)(row_cos + i1);
+  r.s[0] = *(const rp_f32x4*)(row_cos + half + i0), r.s[1] = *(const rp_f32x4*)(row_cos + half + i1);
+  return r;
+}
+__device__ __forceinline__ void rp_turn(const RopeForm& a, const RopeTurn& r, float (&x0)[8], float (&x1)[8]) {
+  if (!a.interleaved) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float u = x0[e], v = x1[e], c = r.c[e / 4][e % 4], sn = r.s[e / 4][e % 4];
+      x0[e] = u * c - v * sn + r.bad;
+      x1[e] = v * c + u * sn + r.bad;
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float(&x)[8] = q ? x1 : x0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float u = x[2 * e], v = x[2 * e + 1], c = r.c[q][e], sn = r.s[q][e];
+        x[2 * e] = u * c - v * sn + r.bad;
+        x[2 * e + 1] = v * c + u * sn + r.bad;
+      }
+    }
+  }
+}
+
+// 1 / sqrt(mean of the squares + eps) of a row; every lane of it takes part.
+template <int LPR>
+__device__ __forceinline__ float rp_inverse(const RopeForm& a, const float (&x0)[8], const float (&x1)[8]) {
+  float sq = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(x0[e], x0[e], __builtin_fmaf(x1[e], x1[e], sq));
+  sq = rp_group_sum<LPR>(sq);
+  return 1.0f / sqrtf(sq / (float)a.d + a.eps);
+}
+
 // Norm (where there are weights) and rotation (turn) of a row at position *pos; every lane of the
 // row's LPR takes part.
 template <int DT, int LPR>
@@ -88,11 +149,7 @@ __device__ __forceinline__ void rp_norm_turn(const RopeForm& a, const RopeLane& 
   const bool pair = l.pair, has0 = l.has0, has1 = l.has1;
   const int c0 = l.c0, c1 = l.c1;
   if (weights) {
-    float sq = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sq = __builtin_fmaf(x0[e], x0[e], __builtin_fmaf(x1[e], x1[e], sq));
-    sq = rp_group_sum<LPR>(sq);
-    const float inv = 1.0f / sqrtf(sq / (float)a.d + a.eps);
+    const float inv = rp_inverse<LPR>(a, x0, x1);
     float w[8];
     if (has0) {
       rp_load8<DT>((const elem*)weights + 8 * c0, w);
@@ -106,34 +163,8 @@ __device__ __forceinline__ void rp_norm_turn(const RopeForm& a, const RopeLane& 
     }
   }
   if (turn && pair) {
-    const int at = *pos, half = a.rot >> 1;
-    const bool known = at >= 0 && at < a.n_pos;
-    const float* row_cos = a.table + (known ? (int64_t)at * a.rot : 0);
-    const float bad = known ? 0.f : __builtin_nanf("");     // a position that the table lacks shows
-    if (!a.interleaved) {
-      float c[8], sn[8];
-      rp_load8<SLH_F32>(row_cos + 8 * p, c);
-      rp_load8<SLH_F32>(row_cos + half + 8 * p, sn);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float u = x0[e], v = x1[e];
-        x0[e] = u * c[e] - v * sn[e] + bad;
-        x1[e] = v * c[e] + u * sn[e] + bad;
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        float(&x)[8] = q ? x1 : x0;
-        const int i0 = 4 * (q ? c1 : c0);
-        const rp_f32x4 c = *(const rp_f32x4*)(row_cos + i0), sn = *(const rp_f32x4*)(row_cos + half + i0);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float u = x[2 * e], v = x[2 * e + 1];
-          x[2 * e] = u * c[e] - v * sn[e] + bad;
-          x[2 * e + 1] = v * c[e] + u * sn[e] + bad;
-        }
-      }
-    }
+    const RopeTurn r = rp_turn_of(a, l, p, *pos);
+    rp_turn(a, r, x0, x1);
   }
 }
 
