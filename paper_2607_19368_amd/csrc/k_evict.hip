@@ -18,6 +18,7 @@
 #include "cache8.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace slh {
 
@@ -49,6 +50,11 @@ __device__ __forceinline__ uint32_t ev_key(float w) {
 }
 // and back
 __device__ __forceinline__ float ev_weight(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+
+// lanes below this one of a mask
+__device__ __forceinline__ int ev_below(unsigned long long m) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
 
 constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64;
 constexpr int EV_BINS = 4096, EV_LIST = 1024;
@@ -82,17 +88,35 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   }
   // rows of this wave, 64 at a time
   const int steps = (n + EV_THREADS - 1) / EV_THREADS, in_lds = min(steps, LDS), row0 = wave * steps * 64 + lane;
-  auto key_of = [&](int i) { return row0 + 64 * i < n ? ev_key(w[row0 + 64 * i]) : 0u; };
-  auto each = [&](auto&& f) __attribute__((always_inline)) {
-#pragma unroll 4
-    for (int i = 0; i < in_lds; ++i) f(row0 + 64 * i, s_key[i * EV_THREADS + tid]);
-#pragma unroll 4
-    for (int i = LDS; i < steps; ++i) f(row0 + 64 * i, key_of(i));
+  // past the end the last again: a load under a branch would be waited for in it
+  auto key_of = [&](int i) {
+    const float x = w[min(row0 + 64 * i, n - 1)];
+    return row0 + 64 * i < n ? ev_key(x) : 0u;
   };
   // candidates: rows [lo, lo + m), of which `need` stay
   const int lo = a.first, m = n - a.last - lo;
   int need = a.budget - a.first - a.last;
   auto is_candidate = [&](int j) { return (unsigned)(j - lo) < (unsigned)m; };
+  // f(whole, row, weight) for this wave's rows; whole: all 64 are candidates
+  auto one = [&](auto&& f, int i, uint32_t k) __attribute__((always_inline)) {
+    const int first = wave * steps * 64 + 64 * i;
+    if (first >= lo && first + 63 < lo + m)
+      f(std::true_type{}, row0 + 64 * i, k);
+    else
+      f(std::false_type{}, row0 + 64 * i, k);
+  };
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll 4
+    for (int i = 0; i < in_lds; ++i) one(f, i, s_key[i * EV_THREADS + tid]);
+    for (int i0 = LDS; i0 < steps; i0 += 8) {
+      uint32_t k[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[e] = key_of(min(i0 + e, steps - 1));
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (i0 + e < steps) one(f, i0 + e, k[e]);
+    }
+  };
   auto clear = [&] {
     for (int i = tid; i < EV_BINS; i += EV_THREADS) s_hist[i] = 0;
     __syncthreads();
@@ -121,20 +145,22 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   };
   // rows that stay for sure, and those with the smallest weight that stays, of which the first `need` do
   uint32_t least = 0xffffffffu;                    // none: behind all of them
-  auto kind = [&](int j, uint32_t k, unsigned long long& same, unsigned long long& sure) __attribute__((always_inline)) {
-    const bool candidate = is_candidate(j);
+  auto kind = [&](auto whole, int j, uint32_t k, unsigned long long& same, unsigned long long& sure) __attribute__((always_inline)) {
+    const bool candidate = decltype(whole)::value || is_candidate(j);
     same = __ballot(candidate && k == least);
     sure = __ballot(candidate ? k > least : j < n);
   };
   clear();
   auto take = [&](int i, uint32_t k) __attribute__((always_inline)) {
     if (i < LDS) s_key[i * EV_THREADS + tid] = k;
-    if (is_candidate(row0 + 64 * i)) atomicAdd(&s_hist[k >> 20], 1);
+    one([&](auto whole, int j, uint32_t) {
+      if (decltype(whole)::value || is_candidate(j)) atomicAdd(&s_hist[k >> 20], 1);
+    }, i, k);
   };
   for (int i0 = 0; i0 < steps; i0 += 8) {
     uint32_t k[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) k[e] = i0 + e < steps ? key_of(i0 + e) : 0u;
+    for (int e = 0; e < 8; ++e) k[e] = key_of(min(i0 + e, steps - 1));
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (i0 + e < steps) take(i0 + e, k[e]);
@@ -148,14 +174,14 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
     if (tid == 0) s_listed = 0;
     __syncthreads();
     uint32_t* const listed = (uint32_t*)s_hist + EV_BINS - 2 * EV_LIST;
-    each([&](int j, uint32_t k) {
-      const bool candidate = is_candidate(j), in = candidate && k >> 20 == top;
+    each([&](auto whole, int j, uint32_t k) {
+      const bool candidate = decltype(whole)::value || is_candidate(j), in = candidate && k >> 20 == top;
       n_sure += __popcll(__ballot(candidate ? k >> 20 > top : j < n));
       const unsigned long long who = __ballot(in);
       if (!who) return;
       int to = 0;
       if (lane == 0) to = atomicAdd(&s_listed, __popcll(who));
-      to = __builtin_amdgcn_readfirstlane(to) + __popcll(who & ((1ull << lane) - 1));
+      to = __builtin_amdgcn_readfirstlane(to) + ev_below(who);
       if (in && to < EV_LIST) listed[to] = k, listed[EV_LIST + to] = wave;
     });
     if (lane == 0) s_sure[wave] = n_sure;
@@ -180,7 +206,7 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
         for (int e = 0; e < EV_LIST / EV_THREADS; ++e)
           if (tid + e * EV_THREADS < many && (mine[e] & above) == prefix) atomicAdd(&s_hist[mine[e] >> shift & 1023], 1);
       } else {
-        each([&](int j, uint32_t k) {
+        each([&](auto, int j, uint32_t k) {
           if (is_candidate(j) && (k & above) == prefix) atomicAdd(&s_hist[k >> shift & 1023], 1);
         });
       }
@@ -198,9 +224,9 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   }
   if (!short_list) {
     n_sure = 0;
-    each([&](int j, uint32_t k) {
+    each([&](auto whole, int j, uint32_t k) {
       unsigned long long same, sure;
-      kind(j, k, same, sure);
+      kind(whole, j, k, same, sure);
       n_same += __popcll(same), n_sure += __popcll(sure);
     });
     __syncthreads();
@@ -214,13 +240,13 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   // weights_out may be the weights: where not all are held, rows are listed first then, and their weights moved a chunk at a
   // time, a chunk's loads before its stores
   const bool all_held = steps <= LDS || a.w != a.w_out;
-  each([&](int j, uint32_t k) {
+  each([&](auto whole, int j, uint32_t k) {
     unsigned long long same, sure;
-    kind(j, k, same, sure);
-    const unsigned long long me = 1ull << lane;
-    const int eq = equal + __popcll(same & (me - 1)), to = done + __popcll(sure & (me - 1)) + min(eq, need);
+    kind(whole, j, k, same, sure);
+    const int eq = equal + ev_below(same), to = done + ev_below(sure) + min(eq, need);
+    const bool stays = (sure >> lane & 1) || ((same >> lane & 1) && eq < need);
     equal += __popcll(same), done += __popcll(sure);
-    if ((sure & me) || ((same & me) && eq < need)) {
+    if (stays) {
       kept[to] = j;
       if (all_held) w_out[to] = ev_weight(k);
     }
