@@ -183,10 +183,9 @@ def slh_kv_evict(k_cache, v_cache, weights, page_table, lens, budget, first=0, l
     behind are as they were, with weights of zero.  Caches [pages, H, page, d] of any element type, or in 8
     bits with k_scale and v_scale.  Returns (weights_out, lens_out, kept): kept [B, H, budget] int32 says which row
     each came from (-1: none); weights_out and lens_out may be weights and lens."""
-    try:
-        dtype, dev = k_cache.dtype, k_cache.get_device()
-    except AttributeError:
-        raise SLHError("k_cache must be a tensor") from None
+    if not isinstance(k_cache, torch.Tensor) or not k_cache.is_cuda:
+        raise SLHError("k_cache must be a device tensor")
+    dtype, dev = k_cache.dtype, k_cache.get_device()
     ln, n = _lens(lens, dev)
     if k_scale is not None or v_scale is not None:
         held, cache, block = _held(k_cache, v_cache, k_scale, v_scale, dev)

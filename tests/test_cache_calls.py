@@ -1,0 +1,451 @@
+"""Calls of the operators of a smaller cache: what is refused, streams, graphs, workspaces, strides, sizes past 32 bits, and a run
+of them together."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import cache_plain as CP
+import paper_2607_19368_amd as P
+from paper_2607_19368_amd import slh as B
+
+gpu = pytest.mark.gpu
+BF, HF, FF = torch.bfloat16, torch.float16, torch.float32
+_A = 4096                                         # an aligned address that nothing reads
+
+
+# ---------------------------------------------------------------- the library's refusals: no GPU work is begun
+APPEND = dict(k=_A, k_st=256, k_sh=128, v=_A, v_st=256, v_sh=128, dtype=B.SLH_BF16, T=4, B=2, H=2, d=128, w=None, eps=1e-6, table=None,
+              n_pos=0, rot=0, pos=None, inter=0, kc=_A, vc=_A, ks=_A, vs=_A, n_pages=8, page=32, block=16, pages=_A, ld=4, most=4,
+              lens=_A, cu=_A, stream=None)
+PAGED = dict(q=_A, q_st=512, q_sh=128, kc=_A, vc=_A, ks=_A, vs=_A, dtype=B.SLH_BF16, n_pages=8, page=32, block=16, B=2, n_q=1, Hq=4,
+             Hkv=2, d=128, pages=_A, ld=4, most=4, lens=_A, pre=_A, prefix=9, scale=0.1, out=_A, o_st=512, o_sh=128, lse=None, ws=_A,
+             ws_bytes=1 << 40, stream=None)
+WEIGHTS = dict(q=_A, q_st=512, q_sh=128, kc=_A, ks=_A, dtype=B.SLH_BF16, n_pages=8, page=32, block=16, Tq=2, B=2, Hq=4, Hkv=2, d=128,
+               pages=_A, ld=4, most=4, lens=_A, cu=_A, lse=_A, scale=0.1, w=_A, ws=_A, ws_bytes=1 << 40, stream=None)
+EVICT = dict(kc=_A, vc=_A, ks=_A, vs=_A, dtype=B.SLH_E4M3, n_pages=8, page=32, block=16, B=2, H=2, d=128, pages=_A, ld=4, most=4,
+             lens=_A, lens_out=_A, w=_A, w_out=_A, budget=20, first=4, last=4, kept=_A, ws=_A, ws_bytes=1 << 40, stream=None)
+SIZES = [dict(d=72), dict(d=0), dict(page=8), dict(page=48), dict(page=1 << 17), dict(block=8), dict(block=24), dict(block=512, page=512),
+         dict(block=64), dict(n_pages=0), dict(n_pages=1 << 30), dict(ld=3), dict(most=-1), dict(B=-1), dict(B=(1 << 20) + 1)]
+BAD = {
+    "slh_kv_append_e4m3": (APPEND, SIZES + [
+        dict(H=0), dict(dtype=3), dict(T=-1), dict(T=1 << 26, cu=_A), dict(T=5, cu=None), dict(k=None), dict(v=_A + 8), dict(k_st=-8),
+        dict(v_sh=4), dict(kc=None), dict(vc=_A + 1), dict(ks=None), dict(vs=None), dict(pages=None), dict(lens=None), dict(w=_A + 2),
+        dict(eps=-1.0), dict(eps=math.nan), dict(table=_A, n_pos=4, rot=128, pos=None), dict(table=_A, n_pos=4, rot=144, pos=_A),
+        dict(rot=16), dict(table=_A + 4, n_pos=4, rot=16, pos=_A), dict(most=1 << 26, ld=1 << 26)]),
+    "slh_attend_paged_e4m3": (PAGED, SIZES + [
+        dict(Hq=5), dict(Hq=0), dict(Hkv=0), dict(dtype=B.SLH_F32), dict(n_q=-1), dict(q=None), dict(q=_A + 2), dict(q_st=-8),
+        dict(q_st=(1 << 24) + 8), dict(o_sh=3), dict(out=None), dict(kc=None), dict(vc=_A + 8), dict(ks=None), dict(vs=None),
+        dict(lens=None), dict(pages=None), dict(pre=None), dict(prefix=-1), dict(prefix=1 << 30), dict(scale=0.0), dict(scale=-1.0),
+        dict(scale=math.nan), dict(scale=math.inf), dict(prefix=32768, ws=None), dict(prefix=32768, ws=_A + 4),
+        dict(prefix=32768, ws_bytes=16)]),
+    "slh_attend_weights": (WEIGHTS, SIZES + [
+        dict(Hq=5), dict(Hkv=0), dict(dtype=B.SLH_F32), dict(Tq=-1), dict(Tq=3, cu=None), dict(q=None), dict(q=_A + 2), dict(q_sh=4),
+        dict(q_st=(1 << 24) + 8), dict(kc=None), dict(kc=_A + 8), dict(lens=None), dict(pages=None), dict(lse=None), dict(w=None),
+        dict(scale=0.0), dict(scale=math.nan), dict(Tq=4096, ws=None), dict(Tq=4096, ws=_A + 8), dict(Tq=4096, ws_bytes=64),
+        dict(ks=None, page=48), dict(ks=None, page=0)]),
+    "slh_kv_evict": (EVICT, SIZES + [
+        dict(H=0), dict(dtype=4), dict(ks=None), dict(vs=None), dict(dtype=B.SLH_BF16), dict(budget=0), dict(budget=-3), dict(first=-1),
+        dict(last=-1), dict(first=15, last=6), dict(kc=None), dict(vc=_A + 8), dict(lens=None), dict(lens_out=None), dict(w=None),
+        dict(w_out=None), dict(kept=None), dict(pages=None), dict(ws=None), dict(ws=_A + 4), dict(ws_bytes=8),
+        dict(dtype=B.SLH_F32, ks=None, vs=None, d=12), dict(dtype=B.SLH_F32, ks=None, vs=None, d=264), dict(budget=1 << 28)]),
+}
+
+
+@pytest.mark.parametrize("name,bad", [(n, b) for n, (_, all_) in BAD.items() for b in all_], ids=str)
+def test_refused_before_any_work(name, bad):
+    good = BAD[name][0]
+    args = dict(good, **bad)
+    if "block" in bad and "page" not in bad and bad["block"] == 64:
+        args["page"] = 32                         # blocks larger than a page
+    assert set(args) == set(good)
+    assert getattr(B.load(), name)(*args.values()) == B.SLH_EINVAL
+
+
+@pytest.mark.parametrize("name", BAD)
+def test_nothing_to_do(name):
+    """Batches without sequences or tokens are done at once, whatever their pointers."""
+    args = dict(BAD[name][0], B=0)
+    args.update({k: 0 for k in ("T", "Tq") if k in args}, stream=None)
+    args = {k: None if v == _A else v for k, v in args.items()}
+    if name == "slh_kv_evict":                    # whether a cache is in 8 bits is said by its scales
+        args.update(ks=_A, vs=_A)
+    if name == "slh_attend_paged_e4m3":
+        args.update(ks=_A, vs=_A, prefix=0)
+    assert getattr(B.load(), name)(*args.values()) == B.SLH_OK
+
+
+def test_workspace_sizes():
+    L = B.load()
+    assert L.slh_kv_evict_workspace(0, 2, 128, B.SLH_E4M3, 20) >= 0
+    for bad in ((-1, 2, 128, 3, 20), (2, 0, 128, 3, 20), (2, 2, 0, 3, 20), (2, 2, 128, 5, 20), (2, 2, 128, 3, 0), (1 << 20, 8, 128, 3, 4096)):
+        assert L.slh_kv_evict_workspace(*bad) == B.SLH_EINVAL
+    assert L.slh_attend_weights_workspace(2, 2, 4, 2, 128, 128) == 0
+    assert L.slh_attend_weights_workspace(4096, 2, 4, 2, 128, 4096) > 0
+    assert L.slh_attend_weights_workspace(-1, 2, 4, 2, 128, 128) == B.SLH_EINVAL
+    assert L.slh_attend_paged_e4m3_workspace(2, 1, 5, 2, 128, 128, 0) == B.SLH_EINVAL
+
+
+# ---------------------------------------------------------------- the binding
+def _state(seed=0, d=64, H=2, Hq=4, page=32, block=16, n=3, width=3, dt=BF, device="cuda"):
+    """A cache in 8 bits and in 16, tables, lengths and tokens of n sequences."""
+    g = torch.Generator()
+    g.manual_seed(seed)
+    total = n * width + 1
+    (kc, ks), (vc, vs) = (CP.held(torch.randn(total, H, page, d, generator=g), block) for _ in range(2))
+    s = dict(kc=kc, vc=vc, ks=ks, vs=vs, k16=CP.values(kc, ks).to(dt), v16=CP.values(vc, vs).to(dt),
+             table=torch.randperm(total, generator=g).int()[:n * width].view(n, width), lens=torch.tensor([70, 33, 96][:n], dtype=torch.int32),
+             k=torch.randn(n, H, d, generator=g).to(dt), v=torch.randn(n, H, d, generator=g).to(dt),
+             q=torch.randn(n, Hq, d, generator=g).to(dt), lse=torch.full((n, Hq), 5.0), w=torch.rand(n, H, width * page, generator=g))
+    return {x: t.to(device) for x, t in s.items()}
+
+
+def _calls(s):
+    """name: (call, the tensors that it writes)"""
+    return {
+        "append": (lambda **kw: P.slh_kv_append_e4m3(s["k"], s["v"], s["kc"], s["vc"], s["ks"], s["vs"], s["table"], s["lens"], **kw),
+                   ["kc", "vc", "ks", "vs"]),
+        "paged": (lambda **kw: s.__setitem__("out", P.slh_attend_paged_e4m3(s["q"], s["kc"], s["vc"], s["ks"], s["vs"], s["table"], s["lens"], **kw)),
+                  ["out"]),
+        "weights": (lambda **kw: P.slh_attend_weights(s["q"], s["kc"], s["table"], s["lens"], s["lse"], s["w"], k_scale=s["ks"], **kw), ["w"]),
+        "weights16": (lambda **kw: P.slh_attend_weights(s["q"], s["k16"], s["table"], s["lens"], s["lse"], s["w"], **kw), ["w"]),
+        "evict": (lambda **kw: s.__setitem__("all", P.slh_kv_evict(s["kc"], s["vc"], s["w"], s["table"], s["lens"], 40, 2, 9, s["ks"], s["vs"],
+                                                                   weights_out=s["w"], lens_out=s["lens"], **kw)),
+                  ["kc", "vc", "ks", "vs", "w", "lens"]),
+        "evict16": (lambda **kw: s.__setitem__("all", P.slh_kv_evict(s["k16"], s["v16"], s["w"], s["table"], s["lens"], 40, 2, 9,
+                                                                     weights_out=s["w"], lens_out=s["lens"], **kw)),
+                    ["k16", "v16", "w", "lens"]),
+    }
+
+
+NAMES = ["append", "paged", "weights", "weights16", "evict", "evict16"]
+
+
+def _bits(t):
+    return t.view({1: torch.uint8, 2: torch.int16, 4: torch.int32}[t.element_size()]).clone()
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_tensors_of_the_host_are_refused(name):
+    with pytest.raises(P.SLHError):
+        _calls(_state(device="cpu"))[name][0]()
+
+
+@gpu
+@pytest.mark.parametrize("name", NAMES)
+def test_on_another_stream(name):
+    s, t = _state(), _state()
+    call, written = _calls(s)[name]
+    call()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    _calls(t)[name][0](stream=side)
+    side.synchronize()
+    for x in written:
+        assert torch.equal(_bits(s[x]), _bits(t[x])), x
+    with torch.cuda.stream(side):
+        u = _state()
+        _calls(u)[name][0]()
+    side.synchronize()
+    for x in written:
+        assert torch.equal(_bits(s[x]), _bits(u[x])), x
+
+
+@gpu
+@pytest.mark.parametrize("name", NAMES)
+def test_captured_and_replayed(name):
+    """Replays on inputs that are written anew between them, against the eager call."""
+    s, fresh = _state(), [_state(i) for i in range(3)]
+    s["out"] = torch.empty_like(s["q"])
+    call, written = _calls(s)[name]
+    if name == "paged":
+        call = lambda: P.slh_attend_paged_e4m3(s["q"], s["kc"], s["vc"], s["ks"], s["vs"], s["table"], s["lens"], out=s["out"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for f in fresh:
+        for x, t in f.items():
+            s[x].copy_(t)
+        graph.replay()
+        torch.cuda.synchronize()
+        torch.zeros(1000, device="cuda").sum().item()
+        _calls(f)[name][0]()
+        for x in written:
+            assert torch.equal(_bits(s[x]), _bits(f[x])), x
+
+
+@gpu
+def test_two_graphs_share_a_workspace():
+    """Evictions of two layers' caches, captured apart with one workspace and replayed in turn, and partial sums of weights alike."""
+    layers = [_state(i, n=1, width=40, page=32) for i in range(2)]
+    for s in layers:
+        s["lens"].fill_(1280)
+        s["q"] = torch.randn(300, 4, 64, generator=torch.Generator().manual_seed(5)).to(BF).cuda()
+        s["lse"] = torch.full((300, 4), 6.0, device="cuda")
+        s["cu"] = torch.tensor([0, 300], dtype=torch.int32, device="cuda")
+    need = max(P.slh_kv_evict_workspace(1, 2, 64, CP.CODE, 700), P.slh_attend_weights_workspace(300, 1, 4, 2, 64, 1280))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    keep = [{x: t.clone() for x, t in s.items()} for s in layers]
+
+    def run(s, workspace):
+        P.slh_attend_weights(s["q"], s["kc"], s["table"], s["lens"], s["lse"], s["w"], cu_q=s["cu"], k_scale=s["ks"], workspace=workspace)
+        P.slh_kv_evict(s["kc"], s["vc"], s["w"], s["table"], s["lens"], 700, 3, 20, s["ks"], s["vs"], weights_out=s["w"], lens_out=s["lens"],
+                       kept=s["kept"], workspace=workspace)
+
+    graphs = []
+    for s in layers:
+        s["kept"] = torch.empty(1, 2, 700, dtype=torch.int32, device="cuda")
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run(s, ws)
+    for turn in range(3):
+        for s, k in zip(layers, keep):
+            for x, t in k.items():
+                s[x].copy_(t)
+        ws.fill_(255 - turn)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for s, k in zip(layers, keep):
+            u = {x: t.clone() for x, t in k.items()}
+            u["kept"] = torch.empty_like(s["kept"])
+            run(u, None)
+            for x in ("kc", "vc", "ks", "vs", "w", "lens", "kept"):
+                assert torch.equal(_bits(s[x]), _bits(u[x])), x
+
+
+@gpu
+@pytest.mark.parametrize("name", NAMES)
+def test_gradients_are_refused(name):
+    for x in {"append": ["k", "v"], "paged": ["q"], "weights": ["q", "lse", "w"], "weights16": ["q", "k16", "lse"], "evict": ["w"],
+              "evict16": ["w", "k16"]}[name]:
+        s = _state()
+        s[x].requires_grad_()
+        with pytest.raises(P.SLHError, match="gradient"):
+            _calls(s)[name][0]()
+
+
+@gpu
+def test_arguments_that_do_not_fit():
+    s = _state()
+    wrong = {
+        "k": lambda t: t[:2], "v": lambda t: t.float(), "kc": lambda t: t.view(torch.uint8), "vc": lambda t: t[:-1],
+        "ks": lambda t: t.view(torch.uint8), "vs": lambda t: t[:, :, :1], "table": lambda t: t.long(), "lens": lambda t: t[:2],
+        "q": lambda t: t.float(), "lse": lambda t: t[:, :3], "w": lambda t: t[..., :-1],
+    }
+    uses = {"append": ["k", "v", "kc", "vc", "ks", "vs", "table", "lens"], "paged": ["q", "kc", "vc", "ks", "vs", "table", "lens"],
+            "weights": ["q", "kc", "ks", "table", "lens", "lse", "w"], "evict": ["kc", "vc", "ks", "vs", "table", "lens", "w"]}
+    for name, which in uses.items():
+        for x in which:
+            t = dict(s, **{x: wrong[x](s[x])})
+            with pytest.raises(P.SLHError):
+                _calls(t)[name][0]()
+    for kw in (dict(budget=0), dict(first=20, last=21), dict(last=-1)):
+        with pytest.raises(P.SLHError):
+            P.slh_kv_evict(s["kc"], s["vc"], s["w"], s["table"], s["lens"], **dict(dict(budget=40), **kw), k_scale=s["ks"], v_scale=s["vs"])
+    with pytest.raises(P.SLHError):
+        P.slh_kv_evict(s["kc"], s["vc"], s["w"], s["table"], s["lens"], 40, k_scale=s["ks"])
+    with pytest.raises(P.SLHError):
+        P.slh_kv_evict(s["kc"], s["vc"], s["w"], s["table"], s["lens"], 40)
+    with pytest.raises(P.SLHError):
+        P.slh_attend_paged_e4m3(s["q"], s["kc"], s["vc"], s["ks"], s["vs"], s["table"], s["lens"], prefix_len=9)
+    with pytest.raises(P.SLHError):
+        P.slh_attend_paged_e4m3(s["q"], s["kc"], s["vc"], s["ks"], s["vs"], s["table"], s["lens"], s["table"][0], 97)
+
+
+@gpu
+def test_strides_and_views():
+    """Tokens, queries and results that are parts of wider rows; page tables with room; single tokens whose strides may be anything."""
+    s, t = _state(n=2), _state(n=2)
+    wide = torch.full((2, 9, 72), 7.0, dtype=BF, device="cuda")
+    wide[:, :2, :64], wide[:, 2:4, :64], wide[:, 4:8, :64] = s["k"], s["v"], s["q"]
+    room = torch.full((2, 7), 1 << 30, dtype=torch.int32, device="cuda")
+    room[:, :3] = s["table"]
+    s.update(k=wide[:, :2, :64], v=wide[:, 2:4, :64], q=wide[:, 4:8, :64], table=room[:, :3])
+    for name in ("append", "weights", "evict"):
+        call, written = _calls(s)[name]
+        call()
+        _calls(t)[name][0]()
+        for x in written:
+            assert torch.equal(_bits(s[x]), _bits(t[x])), (name, x)
+    out = torch.full((2, 5, 72), 7.0, dtype=BF, device="cuda")
+    P.slh_attend_paged_e4m3(s["q"], s["kc"], s["vc"], s["ks"], s["vs"], s["table"], s["lens"], out=out[:, 1:, :64])
+    _calls(t)["paged"][0]()
+    assert torch.equal(out[:, 1:, :64], t["out"])
+    out[:, 1:, :64] = 7.0
+    assert bool((out == 7.0).all())
+    s, t = _state(n=1, Hq=2), _state(n=1, Hq=2)
+    odd = lambda x: x.as_strided(x.shape, (2 ** 25 + 7, *x.stride()[1:]))
+    for x in ("k", "v", "q"):
+        s[x] = odd(s[x])
+    for name in ("append", "paged", "weights"):
+        call, written = _calls(s)[name]
+        call()
+        _calls(t)[name][0]()
+        for x in written:
+            assert torch.equal(_bits(s[x]), _bits(t[x])), (name, x)
+
+
+@gpu
+def test_rows_past_32_bits():
+    """A cache of more than 4 GiB of codes, its last pages in use: append, attention, weights and eviction as in a small one."""
+    page, H, d = 128, 8, 128
+    total = (1 << 32) // (page * H * d) + 40
+    s = _state(3, d=d, H=H, Hq=8, page=page, block=32, n=2, width=2)
+    s["lens"] = torch.tensor([200, 131], dtype=torch.int32, device="cuda")
+    big = {x: torch.zeros((total, *s[x].shape[1:]), dtype=torch.uint8, device="cuda").view(s[x].dtype) for x in ("kc", "vc", "ks", "vs")}
+    n = s["kc"].shape[0]
+    for x, t in big.items():
+        t.view(torch.uint8)[-n:] = s[x].view(torch.uint8)
+    b = dict(s, **big, table=s["table"] + (total - n), w=s["w"].clone(), lens=s["lens"].clone())
+    for name in ("append", "paged", "weights", "evict"):
+        _calls(s)[name][0]()
+        call, written = _calls(b)[name]
+        call()
+        for x in written:
+            got = b[x].view(torch.uint8)[-n:] if x in big else _bits(b[x])
+            assert torch.equal(got, _bits(s[x])), (name, x)
+    assert not bool(b["kc"].view(torch.uint8)[:-n].view(torch.int64).any())
+
+
+@gpu
+def test_page_entries_outside_the_cache():
+    """Nothing outside is read or written; sequences with good pages have their results."""
+    good = _state()
+    s = _state()
+    bad = torch.tensor([-1, 2 ** 31 - 1, 10], dtype=torch.int32, device="cuda")
+    s["table"][1] = bad
+    for name in ("append", "paged", "weights", "evict"):
+        call, written = _calls(s)[name]
+        call()
+        _calls(good)[name][0]()
+        if name == "paged":
+            assert torch.equal(s["out"][[0, 2]], good["out"][[0, 2]])
+        if name == "weights":
+            assert torch.equal(s["w"][[0, 2]], good["w"][[0, 2]])
+        mine = good["table"][[0, 2]].long().flatten()
+        for x in ("kc", "vc", "ks", "vs"):
+            assert torch.equal(_bits(s[x])[mine], _bits(good[x])[mine]), (name, x)
+
+
+@gpu
+def test_again_gives_the_same_bits():
+    g = torch.Generator().manual_seed(4)
+    lens = [1000, 3000, 517, 64]
+    new = [700, 200, 517, 1]
+    pages = [-(-n // 64) for n in lens]
+    order = torch.randperm(sum(pages), generator=g).int()
+    table = torch.zeros(4, max(pages), dtype=torch.int32)
+    at = 0
+    for b, n in enumerate(pages):
+        table[b, :n] = order[at:at + n]
+        at += n
+    kc = torch.randn(sum(pages), 2, 64, 128, generator=g).to(BF).cuda()
+    q = torch.randn(sum(new), 10, 128, generator=g).to(BF).cuda()
+    lse = torch.full((sum(new), 10), 6.0, device="cuda")
+    cu = torch.tensor([0, *new]).cumsum(0).int().cuda()
+    w = [torch.zeros(4, 2, max(pages) * 64, device="cuda") for _ in range(4)]
+    for x in w:
+        P.slh_attend_weights(q, kc, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), lse, x, cu_q=cu)
+    assert all(torch.equal(x, w[0]) for x in w)
+
+
+@gpu
+def test_weights_far_behind_a_context():
+    """Many rows against many more keys: every tile of the runs, whole and shared ones, with keys that no query sees."""
+    for new, lens, Hq, Hkv, dt in (([300], [5000], 7, 1, BF), ([64] * 5, [64, 900, 3000, 65, 1281], 8, 2, HF), ([1500, 3, 900], [1500, 40, 200], 6, 2, BF),
+                                   ([130] * 70, [130 + 13 * b for b in range(70)], 2, 1, BF)):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(len(new))
+        d, page = 64, 64
+        pages = [-(-n // page) for n in lens]
+        table = torch.zeros(len(new), max(pages), dtype=torch.int32)
+        at = 0
+        for b, n in enumerate(pages):
+            table[b, :n] = torch.arange(at, at + n)
+            at += n
+        kc = torch.randn(at, Hkv, page, d, generator=g, device="cuda").to(dt)
+        q = torch.randn(sum(new), Hq, d, generator=g, device="cuda").to(dt)
+        lse = 5 + torch.rand(sum(new), Hq, generator=g, device="cuda")
+        cu = [0]
+        for n in new:
+            cu.append(cu[-1] + n)
+        w = torch.zeros(len(new), Hkv, max(pages) * page, device="cuda")
+        P.slh_attend_weights(q, kc, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), lse, w, cu_q=torch.tensor(cu, dtype=torch.int32).cuda())
+        for b, (n, m) in enumerate(zip(new, lens)):
+            k = kc[table[b, :pages[b]].long().cuda()].transpose(1, 2).flatten(0, 1)[:m].double()
+            limit = torch.arange(n, device="cuda") + m - n + 1
+            hide = torch.arange(m, device="cuda")[None] >= limit[:, None]
+            for h in range(Hkv):
+                want, tol = torch.zeros(m, dtype=torch.float64, device="cuda"), torch.zeros(m, dtype=torch.float64, device="cuda")
+                for i in range(Hq // Hkv):
+                    hq = h * (Hq // Hkv) + i
+                    qq, ll = q[cu[b]:cu[b + 1], hq].double(), lse[cu[b]:cu[b + 1], hq].double()[:, None]
+                    s = qq @ k[:, h].t().contiguous() / 8
+                    p = torch.exp(s - ll).masked_fill(hide, 0.0)
+                    # the error of a weight as in cache_plain.weights
+                    u = 2.0 ** -24
+                    e = 2 * d * u * (qq.abs() @ k[:, h].abs().t().contiguous()) / 8 + 2 * u * (s.abs() + ll.abs()) + 4 * u * (s - ll).abs() + 4 * u
+                    want += p.sum(0)
+                    tol += (p * (e + n * Hq / Hkv * u)).sum(0)
+                got = w[b, h, :m].double()
+                assert bool(((got - want).abs() <= tol).all()), (b, h, float(((got - want).abs() - tol).max()))
+            assert not bool(w[b, :, m:].any())
+
+
+@gpu
+def test_a_decode_that_keeps_its_cache_small():
+    """Append, attention, weights and eviction together, step by step: the cache never holds more than the budget and a step's
+    tokens, and what it holds is what a plain cache of the same choices holds."""
+    import attention_plain as AP
+    g = torch.Generator().manual_seed(11)
+    n, H, Hq, d, page, block, budget = 3, 2, 4, 64, 32, 16, 40
+    width = 2
+    table = torch.randperm(n * width, generator=g).int().view(n, width)
+    kc, vc = (torch.zeros(n * width, H, page, d, dtype=torch.uint8).view(CP.CODE).cuda() for _ in range(2))
+    ks, vs = (torch.zeros(n * width, H, page // block, dtype=torch.uint8).view(CP.SCALE).cuda() for _ in range(2))
+    lens, w = torch.zeros(n, dtype=torch.int32).cuda(), torch.zeros(n, H, width * page).cuda()
+    tab, td = P.slh_rope_table(200, d), table.cuda()
+    wk = torch.ones(d, dtype=BF).cuda()
+    for t in range(90):
+        k, v, q = (torch.randn(n, h, d, generator=g).to(BF).cuda() for h in (H, H, Hq))
+        lens += 1
+        P.slh_kv_append_e4m3(k, v, kc, vc, ks, vs, td, lens, k_weight=wk, table=tab, pos=torch.full((n,), t, dtype=torch.int32).cuda())
+        lse, before = torch.empty(n, Hq).cuda(), w.clone()
+        out = P.slh_attend_paged_e4m3(q, kc, vc, ks, vs, td, lens, lse_out=lse)
+        P.slh_attend_weights(q, kc, td, lens, lse, w, k_scale=ks)
+        m = int(lens[0])
+        assert lens.tolist() == [m] * n and m <= min(t + 1, budget + 20)
+        if t % 9 == 0 or m == budget + 20:
+            K, V = CP.values(kc.cpu(), ks.cpu()), CP.values(vc.cpu(), vs.cpu())
+            for b in range(n):
+                kk, vv = (x[table[b].long()].transpose(1, 2).flatten(0, 1)[:m] for x in (K, V))
+                o, tol, e, etol = AP.attend(q[b:b + 1].cpu(), kk, vv, [m], 1 / 8)
+                assert bool(((out[b].double().cpu() - o[0]).abs() <= tol[0]).all()) and bool(((lse[b].double().cpu() - e[0]).abs() <= etol[0]).all())
+                add, wtol = CP.weights(q[b:b + 1].cpu(), kk, lse[b:b + 1].cpu(), [m], 1 / 8)
+                off = (w[b, :, :m].double().cpu() - before[b, :, :m].double().cpu() - add).abs()
+                assert bool((off <= wtol + 2.0 ** -24 * w[b, :, :m].double().cpu().abs()).all())
+        if m == budget + 20:
+            had, wh = (CP.values(kc.cpu(), ks.cpu()), CP.values(vc.cpu(), vs.cpu())), w.cpu()
+            kept = P.slh_kv_evict(kc, vc, w, td, lens, budget, 4, 8, ks, vs, weights_out=w, lens_out=lens)[2].cpu()
+            now = CP.values(kc.cpu(), ks.cpu()), CP.values(vc.cpu(), vs.cpu())
+            two = CP.bytes_of(ks.cpu()), CP.bytes_of(vs.cpu())
+            for b in range(n):
+                for h in range(H):
+                    stay = CP.keep(wh[b, h].tolist(), m, budget, 4, 8)
+                    assert kept[b, h].tolist() == stay
+                    for x, y, s in zip(had, now, two):
+                        rows = [x[int(table[b, j // page]), h, j % page] for j in stay]
+                        got = [y[int(table[b, i // page]), h, i % page] for i in range(budget)]
+                        steps = [2.0 ** float(s[int(table[b, i // page]), h, i % page // block] - 127 - 10) for i in range(budget)]
+                        # exact, but for codes that become subnormal: half their step, 2^-10 of the power
+                        assert all(bool(((a - c).abs() <= u).all()) for a, c, u in zip(rows, got, steps))
+                    assert torch.equal(w[b, h, :budget].cpu(), wh[b, h, stay])
+    assert int(lens[0]) < budget + 20
+
+
+def test_python_names_are_the_librarys():
+    for name in ("slh_kv_append_e4m3", "slh_attend_paged_e4m3", "slh_attend_weights", "slh_kv_evict"):
+        assert callable(getattr(P, name)) and isinstance(getattr(B.load(), name), ctypes._CFuncPtr)
