@@ -612,7 +612,8 @@ int slh_kv_append_e4m3(const void *k, int64_t k_st, int64_t k_sh, const void *v,
 /*
  * slh_attend_paged against a cache in 8 bits: its sequences, prefix, limits and results, with the codes' values as
  * keys and values.  They are taken into the products in dtype (exact where they lie in its normal range; fp16: magnitudes from
- * 65520 become infinite).  NaN codes that a query does not see do not reach it.
+ * 65520 become infinite).  What a query does not see does not reach it, infinities and NaN included.
+ * Values times weights of up to 2^8 are added up in fp32 before the division: with bf16 values near 2^120 the sums can pass it.
  * workspace: slh_attend_paged_e4m3_workspace() bytes, with max_len = max_pages page_size.
  */
 int64_t slh_attend_paged_e4m3_workspace(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t d,

@@ -206,13 +206,15 @@ __device__ __forceinline__ void rows8(const Attend8Args& A, int block, float* sm
       pf[n] = at_u32x4{TY::pack(p[0], p[1]), TY::pack(p[2], p[3]), TY::pack(p[4], p[5]), TY::pack(p[6], p[7])};
     }
 
-    uint32_t odd = 0;
+    uint32_t odd = 0, past[2];
     if (masked) {
+      past[0] = c8_past<TY>(__builtin_amdgcn_readfirstlane(s.v_two[0]));
+      past[1] = c8_past<TY>(__builtin_amdgcn_readfirstlane(s.v_two[1]));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
 #pragma unroll
-        for (int x = 0; x < X; ++x) odd |= c8_nan(s.v[i][x]);
-        if (R) odd |= c8_nan(s.vr[i]);
+        for (int x = 0; x < X; ++x) odd |= c8_odd(s.v[i][x], past[i / 4]);
+        if (R) odd |= c8_odd(s.vr[i], past[i / 4]);
       }
     }
     // bytes of the keys 2 i and 2 i + 1 side by side, of the d pair q of part x (or of the rest)
@@ -220,18 +222,23 @@ __device__ __forceinline__ void rows8(const Attend8Args& A, int block, float* sm
       return __builtin_amdgcn_perm(c1, c0, q ? 0x07030602u : 0x05010400u);
     };
     if (__builtin_expect(masked && __ballot(odd) != 0, 0)) {
-      // 0 x NaN in the product would reach rows that do not see the key: a product of where the NaN codes are with what
-      // each row sees says which results they reach, and they leave V
+      // 0 x NaN or infinity in the product would reach rows that do not see the key: products of where they are (NaN:
+      // of both signs) with what each row sees say which results they reach, and they leave V
       const uint32_t one = std::is_same<TY, AtBf16>::value ? 0x3f80u : 0x3c00u;
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
-        at_u32x4 bad;
+        at_u32x4 up_here, down_here;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t c0 = b < M ? s.v[2 * i][b / 4 < X ? b / 4 : 0] : s.vr[2 * i];
           const uint32_t c1 = b < M ? s.v[2 * i + 1][b / 4 < X ? b / 4 : 0] : s.vr[2 * i + 1];
           const int at = 8 * (b < M ? b % 4 : b - M) + 7;
-          bad[i] = ((c8_nan(c0) >> at) & 1u) * one | (((c8_nan(c1) >> at) & 1u) * one) << 16;
+          const uint32_t u0 = c8_odd(c0, past[i / 2]) & (c8_odd(c0, 0x01010101u) | ~c0);
+          const uint32_t u1 = c8_odd(c1, past[i / 2]) & (c8_odd(c1, 0x01010101u) | ~c1);
+          const uint32_t d0 = c8_odd(c0, past[i / 2]) & (c8_odd(c0, 0x01010101u) | c0);
+          const uint32_t d1 = c8_odd(c1, past[i / 2]) & (c8_odd(c1, 0x01010101u) | c1);
+          up_here[i] = ((u0 >> at) & 1u) * one | (((u1 >> at) & 1u) * one) << 16;
+          down_here[i] = ((d0 >> at) & 1u) * one | (((d1 >> at) & 1u) * one) << 16;
         }
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -242,19 +249,22 @@ __device__ __forceinline__ void rows8(const Attend8Args& A, int block, float* sm
             const int j = 16 * (i / 2) + 2 * (i % 2);
             sees[i] = (j < left ? one : 0u) | (j + 1 < left ? one : 0u) << 16;
           }
-          at_f32x4 hit[1] = {at_f32x4{0.f, 0.f, 0.f, 0.f}};
-          hit[0] = TY::mfma16(bad, sees, hit[0]);
+          at_f32x4 hit[2] = {at_f32x4{0.f, 0.f, 0.f, 0.f}, at_f32x4{0.f, 0.f, 0.f, 0.f}};
+          hit[0] = TY::mfma16(up_here, sees, hit[0]);
+          hit[1] = TY::mfma16(down_here, sees, hit[1]);
           at_products_done(hit);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (hit[0][e] > 0.f) o[n][b][e] = __builtin_nanf("");
+          for (int e = 0; e < 4; ++e) {
+            if (hit[0][e] > 0.f) o[n][b][e] += INFINITY;
+            if (hit[1][e] > 0.f) o[n][b][e] -= INFINITY;
+          }
         }
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
 #pragma unroll
-        for (int x = 0; x < X; ++x) s.v[i][x] &= ~((c8_nan(s.v[i][x]) >> 7) * 0xffu);
-        if (R) s.vr[i] &= ~((c8_nan(s.vr[i]) >> 7) * 0xffu);
+        for (int x = 0; x < X; ++x) s.v[i][x] &= ~((c8_odd(s.v[i][x], past[i / 4]) >> 7) * 0xffu);
+        if (R) s.vr[i] &= ~((c8_odd(s.vr[i], past[i / 4]) >> 7) * 0xffu);
       }
     }
 #pragma unroll

@@ -48,7 +48,7 @@ def test_every_code_and_power():
     """Codes through attention: one key a sequence with weight 1 gives its value back, for every code and for powers of both ends."""
     d, block = 64, 16
     codes = torch.arange(256, dtype=torch.uint8).view(4, 64)
-    for dt, powers in ((BF, (-100, -7, -1, 0, 3, 100)), (HF, (-5, 0, 7))):
+    for dt, powers in ((BF, (-100, -7, -1, 0, 3, 100)), (HF, (-5, 0, 7, 9))):       # 2^9: past fp16, infinite
         for x in powers:
             kc = torch.zeros(4, 1, 16, d, dtype=torch.uint8).view(CP.CODE).cuda()
             vc = torch.zeros(4, 1, 16, d, dtype=torch.uint8)
@@ -60,6 +60,37 @@ def test_every_code_and_power():
                                           torch.ones(4, dtype=torch.int32).cuda())
             want = (codes.view(CP.CODE).double() * 2.0 ** x).to(dt)
             assert torch.equal(out[:, 0].cpu().nan_to_num(nan=0.5), want.nan_to_num(nan=0.5)), (dt, x)
+
+
+@pytest.mark.parametrize("dt,x", [(HF, 8), (HF, 9), (HF, 14), (HF, 23), (HF, 24), (HF, 30), (BF, 120), (BF, 121), (BF, 127)])
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("n_q", [1, 3, 40])
+def test_values_past_the_type(dt, x, d, n_q):
+    """Infinite values: those that a query sees make its outputs infinite, those behind them (and NaN there) nothing."""
+    page, n = 32, 16 + n_q + 5
+    kc = torch.zeros(2, 1, page, d, dtype=torch.uint8)
+    vc = torch.zeros(2, 1, page, d, dtype=torch.uint8)
+    rows = vc.view(2 * page, d)
+    codes = torch.arange(256, dtype=torch.uint8)
+    rows[n - n_q] = codes[(torch.arange(d) * 3 + 64) % 256]                     # seen by all; the columns' codes differ
+    rows[n - 1] = codes[(torch.arange(d) * 7 + 5) % 256]                        # seen by the last query
+    rows[n:] = codes[(torch.arange(d) * 5 + 1) % 256]                           # unwritten rows, some of them NaN
+    two = torch.full((2, 1, page // 16), 127 + x, dtype=torch.uint8)
+    held = [kc.view(CP.CODE).cuda(), vc.view(CP.CODE).cuda(), torch.full_like(two, 127).view(CP.SCALE).cuda(), two.view(CP.SCALE).cuda()]
+    q = torch.ones(1, n_q, 1, d, dtype=dt).cuda()
+    out = P.slh_attend_paged_e4m3(q, *held, torch.tensor([[0, 1]], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda())[0, :, 0]
+    v = (rows.view(CP.CODE).double() * 2.0 ** x).to(dt).double()                # keys are zeros: every row that is seen has the same weight
+    for i in range(n_q):
+        want = v[:n - n_q + 1 + i].mean(0)
+        got, most = out[i].cpu().double(), v[:n - n_q + 1 + i].nan_to_num(0, 0, 0).abs().mean(0)
+        odd = ~torch.isfinite(want)
+        # the largest weight is 1 before the sums are divided, here every one: finite fp32 sums are those below 2^128, in any
+        # order if those of the magnitudes are
+        whole = most * (n - n_q + 1 + i) < 2.0 ** 128 * (1 - 2.0 ** -16)
+        assert torch.equal(got[odd].nan_to_num(nan=0.5), want[odd].nan_to_num(nan=0.5)), i
+        # weights to half a step, the sum of n terms in fp32, the output to half a step (subnormal fp16: 2^-25)
+        tol = most[~odd] * (torch.finfo(dt).eps + (n + 8) * 2.0 ** -23) + 2.0 ** -25
+        assert bool(((got[~odd] - want[~odd]).abs() <= tol)[whole[~odd]].all()), i
 
 
 # ---------------------------------------------------------------- append
@@ -479,6 +510,12 @@ def test_evict_blocks(page, block, d):
 def test_evict_budgets(budget, first, last):
     _evict_case([600, 20, 19, 21, 1], budget, first, last, 1, 64, BF, 64, 0, budget)
     _evict_case([600, 20, 19, 21, 1], budget, first, last, 1, 64, BF, 64, 16, budget)
+
+
+@pytest.mark.parametrize("n,budget", [(33000, 1500), (60011, 32900), (8193, 8192)])
+def test_evict_long_in_place(n, budget):
+    """More rows than are held at once, their weights moved in place."""
+    _evict_case([n, 17, budget + 1], budget, 3, 11, 1, 64, BF, 64, 0, n, place=True)
 
 
 @pytest.mark.parametrize("block", [0, 64])

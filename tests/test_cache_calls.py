@@ -311,6 +311,28 @@ def test_rows_past_32_bits():
 
 
 @gpu
+def test_weights_where_tiles_pass_31_bits():
+    """A table for 2^29 rows and 140000 queries: the bound of the tiles is past 31 bits, whatever the lengths."""
+    page, most, d, n, T = 65536, 8190, 64, 300, 140000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    kc = torch.randn(1, 1, page, d, generator=g, device="cuda").to(BF)
+    q = torch.randn(T, 1, d, generator=g, device="cuda").to(BF)
+    lse = torch.full((T, 1), 5.0, device="cuda")
+    table = torch.full((1, most), 1 << 30, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    lens, cu = torch.tensor([n], dtype=torch.int32, device="cuda"), torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    w = torch.zeros(1, 1, most * page, device="cuda")
+    P.slh_attend_weights(q, kc, table, lens, lse, w, cu_q=cu)
+    # the last 300 queries see the rows up to their own, those before none
+    small = torch.zeros(1, 1, page, device="cuda")
+    P.slh_attend_weights(q[T - n:], kc, table[:, :1], lens, lse[T - n:], small, cu_q=torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    # the same products and terms in another order of at most 300: sums of positive numbers, 300 2^-24 apart each
+    assert bool(((w[0, 0, :n] - small[0, 0, :n]).abs() <= 2 * n * 2.0 ** -24 * small[0, 0, :n]).all()) and bool((small[0, 0, :n] > 0).all())
+    assert not bool(w[0, 0, n:].any())
+
+
+@gpu
 def test_page_entries_outside_the_cache():
     """Nothing outside is read or written; sequences with good pages have their results."""
     good = _state()
