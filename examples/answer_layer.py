@@ -7,6 +7,10 @@ them (slh_qk_norm_rope, slh_attend).  Keys and values stay in a paged cache (slh
 questions is decoded token by token behind that prefix, which all of them share
 (slh_kv_append, slh_attend_paged).
 
+The same with a smaller cache (run_small): keys and values in 8 bits (slh_kv_append_e4m3,
+slh_attend_paged_e4m3), the document cut to the macro-tokens that its last ones look at most, and each question's own
+tokens to those that received the most attention (slh_attend_weights, slh_kv_evict).
+
     python examples/answer_layer.py [workload] [questions] [tokens each]
 """
 import os
@@ -93,6 +97,71 @@ def run(X, ctx, n_it, layer, questions, rho=None):
     return E, pos, out, torch.stack(steps, 1)
 
 
+def small_cache(layer, pages, device):
+    """Codes of keys and values and their scales, empty."""
+    codes = [torch.zeros((pages, layer.Hkv, PAGE, layer.d), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.full((pages, layer.Hkv, 1), 127, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu) for _ in range(2)]
+    return codes + scales
+
+
+def prefill_small(layer, E, pos, held, pages, budget, window=64):
+    """Attention over a compressed prompt, whose keys and values go to `pages` of a cache in 8 bits; of more than `budget`
+    macro-tokens stay the first 4, the last `window` and those that these look at most.  Returns (output, how many stay)."""
+    q, k, v = layer.project(E)
+    q, k = P.slh_qk_norm_rope(q, k, layer.wq, layer.wk, table=layer.table, pos=pos, q_out=q, k_out=k)
+    M = len(E)
+    lens, table = torch.tensor([M], dtype=torch.int32, device=E.device), pages[None]
+    P.slh_kv_append_e4m3(k, v, *held, table, lens)
+    cu = torch.tensor([0, M], dtype=torch.int32, device=E.device)
+    lse = torch.empty((M, layer.Hq), device=E.device)
+    out = P.slh_attend(q, k, v, cu, lse_out=lse)
+    if M <= budget:
+        return out, M
+    last = min(window, budget - 4)
+    weights = torch.zeros((1, layer.Hkv, len(pages) * PAGE), device=E.device)
+    P.slh_attend_weights(q[None, M - last:], held[0], table, lens, lse[None, M - last:], weights, k_scale=held[2])
+    P.slh_kv_evict(held[0], held[1], weights, table, lens, budget, 4, last, held[2], held[3])
+    return out, budget
+
+
+def decode_small(layer, x, pos, held, table, lens, weights, pages, M, budget, cut):
+    """decode() in 8 bits; `cut`: own tokens are cut to the last 4 and, of `budget` in all, those with the most weight."""
+    q, k, v = layer.project(x)
+    q, _ = P.slh_qk_norm_rope(q, q_weight=layer.wq, table=layer.table, pos=pos, q_out=q)
+    lens += 1
+    P.slh_kv_append_e4m3(k, v, *held, table, lens, k_weight=layer.wk, table=layer.table, pos=pos)
+    lse = torch.empty(q.shape[:2], device=x.device)
+    out = P.slh_attend_paged_e4m3(q, *held, table, lens, pages, M, lse_out=lse)
+    P.slh_attend_weights(q, held[0], table, lens, lse, weights, k_scale=held[2])
+    if cut:
+        P.slh_kv_evict(held[0], held[1], weights, table, lens, budget, 0, 4, held[2], held[3], weights_out=weights, lens_out=lens)
+    return out
+
+
+def run_small(X, ctx, n_it, layer, questions, budget, own_budget, rho=None):
+    """run() with a cache in 8 bits that holds at most `budget` macro-tokens and 2 own_budget own tokens of a question.  Returns (E, positions,
+    macro-tokens kept, prefill output, decode outputs)."""
+    N = X.shape[0]
+    E, pos, _, M, _ = P.compress(ctx, X, n_it, rho)
+    n_seq, n, _ = questions.shape
+    n_pre, n_own = -(-M // PAGE), -(-min(n, 2 * own_budget) // PAGE)
+    held = small_cache(layer, n_pre + n_seq * n_own, X.device)
+    pages = torch.arange(n_pre, dtype=torch.int32, device=X.device)
+    table = (n_pre + torch.arange(n_seq * n_own, dtype=torch.int32, device=X.device)).view(n_seq, n_own)
+    out, M = prefill_small(layer, E, pos, held, pages, budget)
+    lens = torch.zeros(n_seq, dtype=torch.int32, device=X.device)
+    weights = torch.zeros((n_seq, layer.Hkv, n_own * PAGE), device=X.device)
+    steps, own = [], 0
+    for t in range(n):
+        own += 1                                  # every question's own tokens
+        full = own == 2 * own_budget
+        at = torch.full((n_seq,), N + t, dtype=torch.int32, device=X.device)
+        steps.append(decode_small(layer, questions[:, t], at, held, table, lens, weights, pages, M, own_budget, full))
+        if full:
+            own = own_budget
+    return E, pos, M, out, torch.stack(steps, 1)
+
+
 def main():
     from workloads import make_inputs
     name = sys.argv[1] if len(sys.argv) > 1 else "qwen7b"
@@ -116,6 +185,14 @@ def main():
     ms = (time.perf_counter() - t) * 1e3
     print(f"{name}: {wl.N} tokens -> {len(E)} macro-tokens at positions 0..{int(pos[-1])}; prefill {tuple(out.shape)}, "
           f"{n_seq} questions of {n} tokens {tuple(steps.shape)}: {ms:.2f} ms in all")
+    small = lambda: run_small(X, ctx, wl.n_it, layer, questions, max(8, len(E) // 2), 16, rho)
+    small()
+    torch.cuda.synchronize()
+    t = time.perf_counter()
+    M = small()[2]
+    torch.cuda.synchronize()
+    ms = (time.perf_counter() - t) * 1e3
+    print(f"in 8 bits, {M} macro-tokens and at most 32 own tokens of each question kept: {ms:.2f} ms in all")
 
 
 if __name__ == "__main__":
