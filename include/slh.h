@@ -661,9 +661,10 @@ int slh_attend_weights(const void *q, int64_t q_st, int64_t q_sh, const void *k_
  * hold (at least 2^-126), the codes follow, exactly but for those that become subnormal.
  * Rows of pages outside [0, n_pages) are not read or written.  budget >= 1; first + last <= budget;
  * max_pages page_size < 2^29; 2 B H ceil(budget / 256) ceil(bytes of a row / 128) <= 2^22.  workspace: slh_kv_evict_workspace()
- * bytes (aligned to 16, contents need no preparation), which no other call may use until this one has run.
+ * bytes, with max_len = max_pages page_size (aligned to 16, contents need no preparation), which no other call may use until this one has run.
  */
-int64_t slh_kv_evict_workspace(int32_t B, int32_t H, int32_t d, int32_t dtype, int32_t budget);
+int64_t slh_kv_evict_workspace(int32_t B, int32_t H, int32_t d, int32_t dtype, int32_t budget,
+                               int64_t max_len);
 int slh_kv_evict(void *k_cache, void *v_cache, void *k_scale, void *v_scale, int32_t dtype,
                  int64_t n_pages, int32_t page_size, int32_t block, int32_t B, int32_t H, int32_t d,
                  const int32_t *page_table, int64_t ld_pages, int32_t max_pages,

@@ -6,15 +6,24 @@
 // of those that share them (few, as a rule: gathered into a list), of the next and the last ten; then the rows that stay, in
 // their order: of equal weights the first rows.  A block a sequence and head, which reads its weights once: 32 a thread stay
 // in LDS, and only those behind are read in every pass.  A wave holds a run of the rows, so that the list of what stays needs
-// the counts of the waves in front and no more barriers.
+// the counts of the waves in front and no more barriers.  Bound by latency where rows are few (8 sequences of 97 rows, 4 heads:
+// 8 us) and by its one compute unit where they are many: 16384 rows 24 us, of which the counts, one LDS atomic a row, and the
+// list take most.
+//
+// k_evict_count, k_evict_gather, k_evict_list: the same for few long sequences, several blocks each: counts of a run; from all
+// counts the bin, and a run's rows in it and above; from all runs' rows in the bin the smallest that stays, then a run's
+// rows behind those of the runs in front.  Integers throughout, so that the order in which blocks run does not show.  48
+// sequences and heads of up to 49157 rows: 8 + 10 + 19 us, where one block each takes 71.
 //
 // k_evict_move: rows are moved in place, in chunks of 256, a block a chunk.  Row i of the result comes from row
 // kept[i] >= i, so the rows that a chunk overwrites are read by it and by chunks in front of it, no others: a block loads its
 // chunk whole, says so, waits until those in front of it that read what it overwrites have said so, and stores.  Chunks are
 // numbered as their blocks start, and none waits before it has said that its rows are loaded, so what is waited for is always
-// running or done.  Keys and values, and parts of 128 bytes of a row, move independently.  In 8 bits
+// running or done.  Keys and values, and parts of 128 bytes of a row, move independently: 300 MB read and written in 82 us, 3.7
+// TB/s of the 4.7 of a plain copy; a row is 128 bytes in 8 bits, and what stays lies scattered.  In 8 bits
 // a block of the cache gets the smallest power of two for the rows that it now holds, and their codes follow (exact but
 // for codes that become subnormal).
+#include "attend_plan.h"
 #include "cache8.h"
 
 #include <algorithm>
@@ -40,6 +49,12 @@ struct EvictArgs {
   int* loaded;             // [streams][chunks] whether a chunk has been loaded
   int B, budget, first, last;
   int parts, chunks;       // of 128 bytes of a row; of EM_ROWS rows of the result
+  // where several blocks pick of one sequence and head:
+  int runs;                // blocks of a pair
+  uint32_t* key;           // [B][H][max_rows] weights as numbers
+  uint32_t* same;          // [B][H][max_rows] by run: those that share the upper bits of the smallest that stays
+  int* hist;               // [B][H][runs][EV_BINS]
+  int* found;              // [B][H][runs][2] of a run: rows that stay for sure by the upper bits, entries of `same`
 };
 
 // Order of weights as unsigned numbers: NaN the largest, zeros equal.
@@ -58,9 +73,42 @@ __device__ __forceinline__ int ev_below(unsigned long long m) {
 
 constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64;
 constexpr int EV_BINS = 4096, EV_LIST = 1024;
+constexpr int EV_LEAST = 2, EV_RUNS = 8, EV_HELD = 16;     // rows of a thread where several blocks pick; blocks of a pair at most
 
 constexpr int EM_THREADS = 512, EM_PASS = EM_THREADS / 8, EM_N = 4, EM_ROWS = EM_PASS * EM_N;   // 8 lanes a row
 static_assert(EM_ROWS >= C8_BLOCK_MOST, "a chunk holds whole blocks");
+
+// What k_evict_move starts from: rows before; of the chunks to be moved how many have started, and which are loaded.
+__device__ __forceinline__ void ev_start(const EvictArgs& a, int64_t at, int n, int i0, int step) {
+  if (i0 == 0) a.count[at] = n;
+  const int streams = 2 * a.parts;
+  for (int i = i0; i < streams; i += step) a.started[at * streams + i] = 0;
+  for (int i = i0; i < streams * a.chunks; i += step) a.loaded[at * streams * a.chunks + i] = 0;
+}
+
+// The bin at which the counts from the top reach `need`, which becomes how many of that bin stay; a thread four bins.
+__device__ __forceinline__ uint32_t ev_find(const int* hist, int* scan, int* found, int& need) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __syncthreads();
+  int c[4], total = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c[e] = hist[EV_BINS - 1 - (4 * tid + e)], total += c[e];
+  const int upto = c8_wave_scan(total);
+  if (lane == 63) scan[wave] = upto;
+  __syncthreads();
+  int above = upto - total;
+#pragma unroll
+  for (int v = 0; v < EV_WAVES; ++v)
+    if (v < wave) above += scan[v];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (above < need && need <= above + c[e]) found[0] = EV_BINS - 1 - (4 * tid + e), found[1] = need - above;
+    above += c[e];
+  }
+  __syncthreads();
+  need = found[1];
+  return (uint32_t)found[0];
+}
 
 // LDS: weights of a thread that stay in LDS.
 template <int LDS>
@@ -76,11 +124,7 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   const float* const w = a.w + at * a.max_rows;
   float* const w_out = a.w_out + at * a.max_rows;
   int* const kept = a.kept + at * a.budget;
-  if (tid == 0) a.count[at] = n;
-  // of the chunks to be moved: how many have started, and which are loaded
-  const int streams = 2 * a.parts;
-  for (int i = tid; i < streams; i += EV_THREADS) a.started[at * streams + i] = 0;
-  for (int i = tid; i < streams * a.chunks; i += EV_THREADS) a.loaded[at * streams * a.chunks + i] = 0;
+  ev_start(a, at, n, tid, EV_THREADS);
   if (n <= a.budget) {
     for (int i = tid; i < a.budget; i += EV_THREADS) kept[i] = i < n ? i : -1;
     for (int i = tid; i < a.max_rows; i += EV_THREADS) w_out[i] = i < n ? w[i] : 0.f;
@@ -121,28 +165,7 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
     for (int i = tid; i < EV_BINS; i += EV_THREADS) s_hist[i] = 0;
     __syncthreads();
   };
-  // the bin at which the counts from the top reach `need`, and how many of it do; a thread four bins
-  auto find = [&] {
-    __syncthreads();
-    int c[4], total = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) c[e] = s_hist[EV_BINS - 1 - (4 * tid + e)], total += c[e];
-    const int upto = c8_wave_scan(total);
-    if (lane == 63) s_same[wave] = upto;
-    __syncthreads();
-    int above = upto - total;
-#pragma unroll
-    for (int v = 0; v < EV_WAVES; ++v)
-      if (v < wave) above += s_same[v];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (above < need && need <= above + c[e]) s_found[0] = EV_BINS - 1 - (4 * tid + e), s_found[1] = need - above;
-      above += c[e];
-    }
-    __syncthreads();
-    need = s_found[1];
-    return (uint32_t)s_found[0];
-  };
+  auto find = [&] { return ev_find(s_hist, s_same, s_found, need); };
   // rows that stay for sure, and those with the smallest weight that stays, of which the first `need` do
   uint32_t least = 0xffffffffu;                    // none: behind all of them
   auto kind = [&](auto whole, int j, uint32_t k, unsigned long long& same, unsigned long long& sure) __attribute__((always_inline)) {
@@ -271,6 +294,230 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   for (int i = a.budget + tid; i < a.max_rows; i += EV_THREADS) w_out[i] = 0.f;
 }
 
+// ---- several blocks a sequence and head: a run of the rows each ----
+struct EvRun {
+  int64_t at;              // pair
+  int n, run, steps;       // rows of the pair; this block's run, 64 rows a wave and step
+  int begin;               // its first row
+};
+__device__ __forceinline__ EvRun ev_run(const EvictArgs& a) {
+  EvRun r;
+  r.at = blockIdx.x / a.runs, r.run = (int)(blockIdx.x - r.at * a.runs);
+  r.n = min(max(a.lens[r.at / a.H], 0), a.max_rows);
+  r.steps = max(EV_LEAST, (int)(((int64_t)r.n + a.runs * EV_THREADS - 1) / (a.runs * EV_THREADS)));
+  r.begin = (int)min((int64_t)r.n, (int64_t)r.run * r.steps * EV_THREADS);
+  return r;
+}
+__device__ __forceinline__ int ev_run_begin(const EvRun& r, int run) { return (int)min((int64_t)r.n, (int64_t)run * r.steps * EV_THREADS); }
+
+// The rows of a run, whose waves hold runs in turn.  The first EV_HELD of a thread are loaded together, before anything else
+// (in order behind stores they would be waited for with these), and stay in registers; those behind (only where a run has
+// more than 16384 rows) are loaded eight at a time in each pass.
+struct EvRows {
+  const uint32_t* from;
+  int first, row0;         // of the wave, of the thread
+  uint32_t held[EV_HELD];
+  __device__ __forceinline__ EvRows(const EvRun& r, const uint32_t* x) : from(x) {
+    first = r.begin + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * r.steps * 64, row0 = first + (threadIdx.x & 63);
+#pragma unroll
+    for (int e = 0; e < EV_HELD; ++e) held[e] = at(r, e);
+  }
+  __device__ __forceinline__ uint32_t at(const EvRun& r, int i) const {   // past the end the last row
+    return from[min((int64_t)row0 + 64 * (int64_t)min(i, r.steps - 1), (int64_t)r.n - 1)];
+  }
+  // f(whole, row, value); whole: all 64 of the wave's step are candidates, rows [lo, lo + m)
+  template <class F>
+  __device__ __forceinline__ void each(const EvRun& r, int lo, int m, F&& f) const {
+    auto one = [&](int i, uint32_t k) __attribute__((always_inline)) {
+      if (first + 64 * i >= lo && first + 64 * i + 63 < lo + m)
+        f(std::true_type{}, row0 + 64 * i, k);
+      else
+        f(std::false_type{}, row0 + 64 * i, k);
+    };
+#pragma unroll
+    for (int e = 0; e < EV_HELD; ++e)
+      if (e < r.steps && first + 64 * e < r.n) one(e, held[e]);
+    for (int i0 = EV_HELD; i0 < r.steps && first + 64 * i0 < r.n; i0 += 8) {
+      uint32_t k[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k[e] = at(r, i0 + e);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (i0 + e < r.steps) one(i0 + e, k[e]);
+    }
+  }
+};
+
+// counts of the upper twelve bits, and the weights as numbers: weights_out may be the weights
+__global__ __launch_bounds__(EV_THREADS) void k_evict_count(EvictArgs a) {
+  __shared__ int s_hist[EV_BINS];
+  const int tid = threadIdx.x;
+  const EvRun r = ev_run(a);
+  ev_start(a, r.at, r.n, r.run * EV_THREADS + tid, a.runs * EV_THREADS);
+  if (r.begin >= r.n) return;
+  const EvRows rows(r, (const uint32_t*)(a.w + r.at * a.max_rows));
+  for (int i = tid; i < EV_BINS; i += EV_THREADS) s_hist[i] = 0;
+  __syncthreads();
+  const int lo = a.first, m = r.n - a.last - lo;
+  uint32_t* const key = a.key + r.at * a.max_rows;
+  rows.each(r, lo, m, [&](auto whole, int j, uint32_t x) {
+    const uint32_t k = ev_key(__uint_as_float(x));
+    if (decltype(whole)::value || j < r.n) key[j] = k;
+    if (decltype(whole)::value || (unsigned)(j - lo) < (unsigned)m) atomicAdd(&s_hist[k >> 20], 1);
+  });
+  __syncthreads();
+  int4* const to = (int4*)(a.hist + (r.at * a.runs + r.run) * EV_BINS);
+  for (int i = tid; i < EV_BINS / 4; i += EV_THREADS) to[i] = ((const int4*)s_hist)[i];
+}
+
+// The bin in which the smallest that stays lies, and `need` as by ev_find.
+__device__ __forceinline__ uint32_t ev_top(const EvictArgs& a, const EvRun& r, int* hist, int* scan, int* found, int& need) {
+  static_assert(EV_BINS == 4 * EV_THREADS, "four bins a thread");
+  int4 sum = make_int4(0, 0, 0, 0);
+  const int4* const from = (const int4*)(a.hist + r.at * a.runs * EV_BINS) + threadIdx.x;
+  const int runs = (int)(((int64_t)r.n + r.steps * EV_THREADS - 1) / (r.steps * EV_THREADS));
+#pragma unroll 4
+  for (int v = 0; v < runs; ++v) {
+    const int4 x = from[v * EV_THREADS];
+    sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+  }
+  ((int4*)hist)[threadIdx.x] = sum;
+  return ev_find(hist, scan, found, need);
+}
+
+// a run's candidates in that bin, in any order, and its rows that stay for sure
+__global__ __launch_bounds__(EV_THREADS) void k_evict_gather(EvictArgs a) {
+  __shared__ int s_hist[EV_BINS];
+  __shared__ int s_scan[EV_WAVES], s_found[2], s_listed, s_sure;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const EvRun r = ev_run(a);
+  int need = a.budget - a.first - a.last;
+  if (r.begin >= r.n || r.n <= a.budget || need == 0) return;
+  const EvRows rows(r, a.key + r.at * a.max_rows);
+  if (tid == 0) s_listed = 0, s_sure = 0;
+  const uint32_t top = ev_top(a, r, s_hist, s_scan, s_found, need);
+  const int lo = a.first, m = r.n - a.last - lo;
+  uint32_t* const same = a.same + r.at * a.max_rows + r.begin;
+  int n_sure = 0;
+  rows.each(r, lo, m, [&](auto whole, int j, uint32_t k) {
+    const bool candidate = decltype(whole)::value || (unsigned)(j - lo) < (unsigned)m, in = candidate && k >> 20 == top;
+    n_sure += __popcll(__ballot(candidate ? k >> 20 > top : j < r.n));
+    const unsigned long long who = __ballot(in);
+    if (!who) return;
+    int to = 0;
+    if (lane == 0) to = atomicAdd(&s_listed, __popcll(who));
+    to = __builtin_amdgcn_readfirstlane(to) + ev_below(who);
+    if (in) same[to] = k;
+  });
+  if (lane == 0 && n_sure) atomicAdd(&s_sure, n_sure);
+  __syncthreads();
+  if (tid < 2) a.found[(r.at * a.runs + r.run) * 2 + tid] = tid ? s_listed : s_sure;
+}
+
+// the smallest that stays, from all runs' lists; a run's rows that stay, behind those of the runs in front of it
+__global__ __launch_bounds__(EV_THREADS) void k_evict_list(EvictArgs a) {
+  __shared__ int s_hist[EV_BINS];
+  __shared__ int s_scan[EV_WAVES], s_found[2], s_front[2], s_same[EV_WAVES], s_sure[EV_WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const EvRun r = ev_run(a);
+  const float* const w = a.w + r.at * a.max_rows;
+  float* const w_out = a.w_out + r.at * a.max_rows;
+  int* const kept = a.kept + r.at * a.budget;
+  const int i0 = r.run * EV_THREADS + tid, step = a.runs * EV_THREADS;
+  if (r.n <= a.budget) {
+    for (int i = i0; i < a.budget; i += step) kept[i] = i < r.n ? i : -1;
+    for (int i = i0; i < a.max_rows; i += step) w_out[i] = i < r.n ? w[i] : 0.f;
+    return;
+  }
+  auto clear = [&] {
+    for (int i = a.budget + i0; i < a.max_rows; i += step) w_out[i] = 0.f;
+  };
+  if (r.begin >= r.n) return clear();
+  const int lo = a.first, m = r.n - a.last - lo;
+  const EvRows rows(r, a.key + r.at * a.max_rows);
+  int need = a.budget - a.first - a.last;
+  uint32_t least = 0xffffffffu;                    // none: behind all of them
+  int done = 0, equal = 0;                         // rows in front of the run that stay for sure, and that are equal to the least
+  if (need > 0) {
+    const uint32_t top = ev_top(a, r, s_hist, s_scan, s_found, need);
+    const int runs = (int)(((int64_t)r.n + r.steps * EV_THREADS - 1) / (r.steps * EV_THREADS));
+    const int* const found = a.found + r.at * a.runs * 2;
+    // f(value) for what the runs' lists hold: the first of a thread of each are loaded together, and stay in registers
+    int many[EV_RUNS];
+    uint32_t held[EV_RUNS];
+#pragma unroll
+    for (int v = 0; v < EV_RUNS; ++v) many[v] = found[2 * min(v, runs - 1) + 1];
+#pragma unroll
+    for (int v = 0; v < EV_RUNS; ++v)
+      held[v] = a.same[r.at * a.max_rows + ev_run_begin(r, min(v, runs - 1)) + min(tid, max(many[v] - 1, 0))];
+    auto lists = [&](int upto, auto&& f) {
+#pragma unroll
+      for (int v = 0; v < EV_RUNS; ++v) {
+        if (v >= upto) break;
+        if (tid < many[v]) f(held[v]);
+        const uint32_t* const list = a.same + r.at * a.max_rows + ev_run_begin(r, v);
+        for (int i = tid + EV_THREADS; i < many[v]; i += EV_THREADS) f(list[i]);
+      }
+    };
+    uint32_t prefix = top << 20;
+#pragma unroll 1
+    for (int shift = 10; shift >= 0; shift -= 10) {
+      const uint32_t above = ~0u << (shift + 10);
+      for (int i = tid; i < EV_BINS; i += EV_THREADS) s_hist[i] = 0;
+      __syncthreads();
+      lists(runs, [&](uint32_t k) {
+        if ((k & above) == prefix) atomicAdd(&s_hist[k >> shift & 1023], 1);
+      });
+      prefix |= ev_find(s_hist, s_scan, s_found, need) << shift;
+    }
+    least = prefix;
+    if (tid < 2) s_front[tid] = 0;
+    __syncthreads();
+    int more = 0, same = 0;                        // lane 0's are the wave's: it has an entry where any lane has
+    lists(r.run, [&](uint32_t k) { more += __popcll(__ballot(k > least)), same += __popcll(__ballot(k == least)); });
+    if (lane == 0 && more) atomicAdd(&s_front[0], more);
+    if (lane == 0 && same) atomicAdd(&s_front[1], same);
+    __syncthreads();
+    done = s_front[0], equal = s_front[1];
+    for (int v = 0; v < r.run; ++v) done += found[2 * v];
+  } else {
+    done = min(r.begin, a.first) + max(0, r.begin - (r.n - a.last));
+  }
+  auto kind = [&](auto whole, int j, uint32_t k, unsigned long long& same, unsigned long long& sure) __attribute__((always_inline)) {
+    const bool candidate = decltype(whole)::value || (unsigned)(j - lo) < (unsigned)m;
+    same = __ballot(candidate && k == least);
+    sure = __ballot(candidate ? k > least : j < r.n);
+  };
+  int n_same = 0, n_sure = 0;
+  rows.each(r, lo, m, [&](auto whole, int j, uint32_t k) {
+    unsigned long long same, sure;
+    kind(whole, j, k, same, sure);
+    n_same += __popcll(same), n_sure += __popcll(sure);
+  });
+  if (lane == 0) s_same[wave] = n_same, s_sure[wave] = n_sure;
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < EV_WAVES; ++v)
+    if (v < wave) equal += s_same[v], done += s_sure[v];
+  rows.each(r, lo, m, [&](auto whole, int j, uint32_t k) {
+    unsigned long long same, sure;
+    kind(whole, j, k, same, sure);
+    const int eq = equal + ev_below(same), to = done + ev_below(sure) + min(eq, need);
+    if ((sure >> lane & 1) || ((same >> lane & 1) && eq < need)) kept[to] = j, w_out[to] = ev_weight(k);
+    equal += __popcll(same), done += __popcll(sure);
+  });
+  clear();
+}
+
+// Blocks that pick of a sequence and head: as many as find a compute unit each, where a table holds so many rows that three
+// launches and what passes between them cost less than one block's time.  One block and several, whole calls (budget 512, 8 to 64
+// sequences and heads): 8192 rows 30-32 and 37-44 us, 16384 rows 40-41 and 41-47, 49152 rows 74-77 and 47-59, 131072 rows 230-243
+// and 61-88; 128 sequences and heads, two blocks each: 49152 rows 81 and 72; 256: 91 and 111.
+inline int ev_runs(int64_t pairs, int64_t max_rows) {
+  if (max_rows <= 16 * EV_THREADS || pairs < 1) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(EV_RUNS, attend_cus() / pairs));
+}
+
 inline int ev_row_bytes(int d, int dtype) { return d * (dtype == SLH_E4M3 ? 1 : dtype == SLH_F32 ? 4 : 2); }
 inline int ev_parts(int d, int dtype) { return (ev_row_bytes(d, dtype) + 127) / 128; }
 
@@ -390,12 +637,15 @@ __global__ __launch_bounds__(EM_THREADS) void k_evict_move(EvictArgs a) {
 
 extern "C" {
 
-int64_t slh_kv_evict_workspace(int32_t B, int32_t H, int32_t d, int32_t dtype, int32_t budget) {
+int64_t slh_kv_evict_workspace(int32_t B, int32_t H, int32_t d, int32_t dtype, int32_t budget, int64_t max_len) {
   using namespace slh;
   if (B < 0 || B > (1 << 20) || H < 1 || H > 65535 || d < 1 || d > 256 || budget < 1) return SLH_EINVAL;
+  if (max_len < 0 || max_len > INT32_MAX / 4) return SLH_EINVAL;
   if (dtype != SLH_BF16 && dtype != SLH_F16 && dtype != SLH_F32 && dtype != SLH_E4M3) return SLH_EINVAL;
   const int64_t chunks = ((int64_t)budget + EM_ROWS - 1) / EM_ROWS, streams = 2 * (int64_t)B * H * ev_parts(d, dtype);
-  return streams * chunks > (1 << 22) ? SLH_EINVAL : 4 * ((int64_t)B * H + streams * (1 + chunks));
+  if (streams * chunks > (1 << 22)) return SLH_EINVAL;
+  const int64_t pairs = (int64_t)B * H, runs = ev_runs(pairs, max_len);
+  return 4 * (pairs + streams * (1 + chunks)) + (runs > 1 ? 4 * pairs * (runs * (EV_BINS + 2) + 2 * max_len) : 0);
 }
 
 int slh_kv_evict(void* k_cache, void* v_cache, void* k_scale, void* v_scale, int32_t dtype, int64_t n_pages, int32_t page_size,
@@ -404,13 +654,14 @@ int slh_kv_evict(void* k_cache, void* v_cache, void* k_scale, void* v_scale, int
                  int32_t first, int32_t last, int32_t* kept, void* workspace, int64_t workspace_bytes, void* stream) {
   using namespace slh;
   const bool e8 = dtype == SLH_E4M3;
-  const int64_t need = slh_kv_evict_workspace(B, H, d, dtype, budget);
+  if (max_pages < 0 || page_size < 1) return SLH_EINVAL;
+  const int64_t need = slh_kv_evict_workspace(B, H, d, dtype, budget, (int64_t)max_pages * page_size);
   if (need < 0 || e8 != (k_scale != nullptr) || e8 != (v_scale != nullptr)) return SLH_EINVAL;
   if (e8 ? d != 64 && d != 80 && d != 96 && d != 128 : d % 8 != 0) return SLH_EINVAL;
-  if (page_size < 1 || page_size > 65536 || (page_size & (page_size - 1))) return SLH_EINVAL;
+  if (page_size > 65536 || (page_size & (page_size - 1))) return SLH_EINVAL;
   if (n_pages < 1 || n_pages > INT32_MAX || n_pages * H > INT32_MAX / page_size) return SLH_EINVAL;
   if (e8 && !c8_sizes_ok(n_pages, page_size, H, block)) return SLH_EINVAL;
-  if (max_pages < 0 || ld_pages < max_pages || (int64_t)max_pages * page_size > INT32_MAX / 4) return SLH_EINVAL;
+  if (ld_pages < max_pages) return SLH_EINVAL;
   if (first < 0 || last < 0 || (int64_t)first + last > budget) return SLH_EINVAL;
   if (B == 0) return SLH_OK;
   if (((uintptr_t)k_cache | (uintptr_t)v_cache) % 16 != 0 || !k_cache || !v_cache || !lens || !lens_out || !kept ||
@@ -425,18 +676,30 @@ int slh_kv_evict(void* k_cache, void* v_cache, void* k_scale, void* v_scale, int
   a.lg_block = e8 ? __builtin_ctz((unsigned)block) : 0;
   a.pages = page_table, a.ld_pages = ld_pages, a.max_rows = max_pages * page_size;
   a.lens = lens, a.lens_out = lens_out, a.w = weights, a.w_out = weights_out, a.kept = kept;
-  a.count = (int*)workspace, a.started = a.count + (int64_t)B * H, a.loaded = a.started + 2 * (int64_t)B * H * a.parts;
+  const int64_t n_pairs = (int64_t)B * H;
+  a.runs = ev_runs(n_pairs, a.max_rows);
+  a.hist = (int*)workspace;
+  a.key = (uint32_t*)(a.hist + (a.runs > 1 ? n_pairs * a.runs * EV_BINS : 0));
+  a.same = a.key + (a.runs > 1 ? n_pairs * a.max_rows : 0);
+  a.found = (int*)(a.same + (a.runs > 1 ? n_pairs * a.max_rows : 0));
+  a.count = a.found + (a.runs > 1 ? n_pairs * a.runs * 2 : 0), a.started = a.count + (int64_t)B * H, a.loaded = a.started + 2 * (int64_t)B * H * a.parts;
   a.B = B, a.budget = budget, a.first = first, a.last = last;
   // a sequence is cut to `budget` only if the table holds more
   a.chunks = (int)(((int64_t)std::min(budget, a.max_rows) + EM_ROWS - 1) / EM_ROWS);
   const dim3 pairs((unsigned)(B * H)), blocks((unsigned)(B * H * 2 * a.parts * std::max(1, a.chunks)));
   hipStream_t s = (hipStream_t)stream;
   (void)hipGetLastError();
-  // 4 KB of LDS for 1024 rows; the smaller kernel leaves room for a second block on a compute unit
-  if (a.max_rows <= 8 * EV_THREADS)
+  if (a.runs > 1) {
+    const dim3 all((unsigned)(B * H * a.runs));
+    hipLaunchKernelGGL(k_evict_count, all, dim3(EV_THREADS), 0, s, a);
+    hipLaunchKernelGGL(k_evict_gather, all, dim3(EV_THREADS), 0, s, a);
+    hipLaunchKernelGGL(k_evict_list, all, dim3(EV_THREADS), 0, s, a);
+  } else if (a.max_rows <= 8 * EV_THREADS) {
+    // 4 KB of LDS for 1024 rows; the smaller kernel leaves room for a second block on a compute unit
     hipLaunchKernelGGL(k_evict_pick<8>, pairs, dim3(EV_THREADS), 0, s, a);
-  else
+  } else {
     hipLaunchKernelGGL(k_evict_pick<32>, pairs, dim3(EV_THREADS), 0, s, a);
+  }
   if (hipGetLastError() != hipSuccess) return SLH_EHIP;
   if (e8)
     hipLaunchKernelGGL(k_evict_move<true>, blocks, dim3(EM_THREADS), 0, s, a);

@@ -540,10 +540,14 @@ struct WeightPlan {
   int runs;
   int64_t bytes;
 };
-static WeightPlan weights_plan(int64_t Tq, int B, int Hkv, int g) {
+//
+// By rows of a sequence.  Few rows and tiles, 4 key/value heads of 7 and 8 of 4: 56 and 64 rows of 8 sequences of 32768 keys
+// 65 and 89, 134 and 177 us; 112 and 128 rows 93 and 89, 201 and 174; 448 and 256 rows 272 and 191, 334 and 233; of 4096
+// keys, 56 and 448 rows: 13 and 21, 49 and 35 us.  Where the sequences' numbers differ, one may have nearly all rows (4000 of 64
+// sequences' 4063 are 63 a sequence), which are far slower by few: tiles from the smaller number on, that loses at most 2.1 times.
+static WeightPlan weights_plan(int64_t Tq, int B, int Hkv, int g, bool even) {
   WeightPlan p = {};
-  // rows of a sequence where they are equal
-  p.tiles = Tq * g > 32 * (int64_t)B;
+  p.tiles = Tq * g > (even ? 96 : 32) * (int64_t)B;
   if (!p.tiles) return p;
   p.runs = std::max(1, 2 * attend_cus() / Hkv);
   p.bytes = p.runs > 1 ? 8 * (int64_t)p.runs * Hkv * WT_BLOCK_KEYS : 0;
@@ -563,7 +567,7 @@ extern "C" {
 int64_t slh_attend_weights_workspace(int64_t Tq, int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int64_t max_len) {
   using namespace slh;
   if (!weights_sizes_ok(Tq, B, Hq, Hkv, d, max_len)) return SLH_EINVAL;
-  return weights_plan(Tq, B, Hkv, Hq / Hkv).bytes;
+  return weights_plan(Tq, B, Hkv, Hq / Hkv, false).bytes;
 }
 
 int slh_attend_weights(const void* q, int64_t q_st, int64_t q_sh, const void* k_cache, const void* k_scale, int32_t dtype,
@@ -582,7 +586,7 @@ int slh_attend_weights(const void* q, int64_t q_st, int64_t q_sh, const void* k_
   if (B == 0 || Tq == 0 || max_pages == 0) return SLH_OK;
   if (!attend_rows_ok(q, q_st, q_sh) || !attend_rows_ok(k_cache, 0, 0) || !page_table || !lens || !lse || !weights)
     return SLH_EINVAL;
-  const WeightPlan p = weights_plan(Tq, B, Hkv, Hq / Hkv);
+  const WeightPlan p = weights_plan(Tq, B, Hkv, Hq / Hkv, !cu_q);
   if (p.bytes && (!workspace || ((uintptr_t)workspace) % 16 != 0 || workspace_bytes < p.bytes)) return SLH_EINVAL;
   WeightArgs a = {};
   a.q = (const uint16_t*)q, a.q_st = q_st, a.q_sh = q_sh;

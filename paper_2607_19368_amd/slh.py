@@ -103,7 +103,7 @@ def load():
         "slh_attend_weights_workspace": (i64, [i64, i32, i32, i32, i32, i64]),
         "slh_attend_weights": (i32, [vp, i64, i64, vp, vp, i32, i64, i32, i32, i64, i32, i32, i32, i32, vp, i64, i32, vp, vp,
                                      vp, f64, vp, vp, i64, vp]),
-        "slh_kv_evict_workspace": (i64, [i32, i32, i32, i32, i32]),
+        "slh_kv_evict_workspace": (i64, [i32, i32, i32, i32, i32, i64]),
         "slh_kv_evict": (i32, [vp, vp, vp, vp, i32, i64, i32, i32, i32, i32, i32, vp, i64, i32, vp, vp, vp, vp, i32, i32, i32,
                                vp, vp, i64, vp]),
     }

@@ -525,6 +525,37 @@ def test_evict_long(n, budget, block):
     _evict_case([n, 17], budget, 0, 0, 2, 64, BF, 64, block, n)
 
 
+def _few(n, seed):
+    """Weights of a sequence of n rows: few of them equal (spread), all of one upper part, NaN, all zeros."""
+    g = _gen(seed)
+    w = torch.stack([torch.randn(n, generator=g), 1 + torch.rand(n, generator=g) * 2.0 ** -6,
+                     torch.where(torch.rand(n, generator=g) < 0.3, float("nan"), 2.0), torch.zeros(n)])
+    return w[:, None].contiguous()
+
+
+@pytest.mark.parametrize("n,budget,first,last", [(16385, 16384, 0, 0), (16448, 2000, 4, 700), (20000, 37, 20, 17), (40000, 33000, 0, 9), (49157, 12301, 4, 256),
+                                                 (140003, 900, 10, 50), (140003, 60000, 50000, 3)])
+@pytest.mark.parametrize("place", [False, True])
+def test_evict_by_runs(n, budget, first, last, place):
+    """Few long sequences: several blocks pick of each; runs that end inside one another's waves, rows kept at both ends."""
+    page = 64
+    w = torch.zeros(4, 1, (-(-n // page) + 1) * page)
+    w[:, :, :n] = _few(n, n)
+    _evict_case([n, n - 1, budget + 1, budget], budget, first, last, 1, 8, BF, page, 0, n, w=w, place=place)
+
+
+@pytest.mark.parametrize("n", [16390, 33000])
+def test_evict_many_long_tables(n):
+    """More sequences than compute units: a block each, which holds 32768 rows of weights or fewer than the sequence has."""
+    _evict_case([n, n - 77] + [31, 1, 0] * 90, 30, 1, 3, 1, 8, BF, 64, 0, n, place=True)
+
+
+@pytest.mark.parametrize("n", [17000, 70000])
+def test_evict_runs_of_a_long_run(n):
+    """Two blocks a sequence, with rows behind those that they hold."""
+    _evict_case([n, 2 * n + 1000] + [600, 40] * 58, 500, 1, 3, 1, 8, BF, 64, 0, n)
+
+
 def test_evict_weights_of_all_kinds():
     """Infinities, NaN of both signs, zeros of both signs, negative ones, the smallest and largest numbers."""
     kinds = torch.tensor([math.inf, -math.inf, math.nan, -math.nan, 0.0, -0.0, -1.0, 1.0, 1e-45, -1e-45, 3.4e38, -3.4e38, 1.0000001])

@@ -78,8 +78,9 @@ def test_nothing_to_do(name):
 
 def test_workspace_sizes():
     L = B.load()
-    assert L.slh_kv_evict_workspace(0, 2, 128, B.SLH_E4M3, 20) >= 0
-    for bad in ((-1, 2, 128, 3, 20), (2, 0, 128, 3, 20), (2, 2, 0, 3, 20), (2, 2, 128, 5, 20), (2, 2, 128, 3, 0), (1 << 20, 8, 128, 3, 4096)):
+    assert L.slh_kv_evict_workspace(0, 2, 128, B.SLH_E4M3, 20, 4096) >= 0
+    for bad in ((-1, 2, 128, 3, 20, 64), (2, 0, 128, 3, 20, 64), (2, 2, 0, 3, 20, 64), (2, 2, 128, 5, 20, 64), (2, 2, 128, 3, 0, 64),
+                (1 << 20, 8, 128, 3, 4096, 64), (2, 2, 128, 3, 20, -1), (2, 2, 128, 3, 20, 1 << 29)):
         assert L.slh_kv_evict_workspace(*bad) == B.SLH_EINVAL
     assert L.slh_attend_weights_workspace(2, 2, 4, 2, 128, 128) == 0
     assert L.slh_attend_weights_workspace(4096, 2, 4, 2, 128, 4096) > 0
@@ -185,7 +186,7 @@ def test_two_graphs_share_a_workspace():
         s["q"] = torch.randn(300, 4, 64, generator=torch.Generator().manual_seed(5)).to(BF).cuda()
         s["lse"] = torch.full((300, 4), 6.0, device="cuda")
         s["cu"] = torch.tensor([0, 300], dtype=torch.int32, device="cuda")
-    need = max(P.slh_kv_evict_workspace(1, 2, 64, CP.CODE, 700), P.slh_attend_weights_workspace(300, 1, 4, 2, 64, 1280))
+    need = max(P.slh_kv_evict_workspace(1, 2, 64, CP.CODE, 700, 1280), P.slh_attend_weights_workspace(300, 1, 4, 2, 64, 1280))
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
     keep = [{x: t.clone() for x, t in s.items()} for s in layers]
 
