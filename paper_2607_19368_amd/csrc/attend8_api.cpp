@@ -4,9 +4,16 @@
 
 namespace slh {
 
-// As ATTEND_COSTS, for the kernels of 8-bit keys.
+// As ATTEND_COSTS, for the kernels of 8-bit keys: steps of 16 and of 32 rows against few keys take less than those of 16-bit keys,
+// whose loads they wait for.  us a call by the costs of 16-bit keys and by these:
+//   8 sequences, prefix 1000, own 100, 28 / 4 heads          18.3   12.6 (in front of each sequence's own keys)
+//   2, 40 new tokens each, own 4000, 40 / 8                   29.3   25.8 (blocks of 32 rows, not 128)
+//   32, 5 new tokens, own 1500, 28 / 4                        20.6   18.1 (32, not 16)
+//   8, own 8000, 28 / 4                                       17.9   16.3
+// 13 other shapes (1 to 256 sequences): 0.93 to 1.02 of the time.  Against every choice of rows and splits in turn, on ten shapes, the
+// plan's time is 1.06 of the best at most.
 static const AttendCost ATTEND8_COSTS[3] = {
-    {16, 1.8, 0.65, 0.8, 0.33}, {32, 2.5, 0.75, 0.95, 0.42}, {AT_ROWS, 3.0, 1.13, 1.75, 0.95}};
+    {16, 1.8, 0.5, 0.63, 0.33}, {32, 2.5, 0.5, 0.65, 0.4}, {AT_ROWS, 3.0, 1.13, 1.75, 0.95}};
 static const AttendKind ATTEND_8 = {ATTEND8_COSTS, 3, 1.0};
 
 static bool attend8_sizes_ok(int B, int n_q, int Hq, int Hkv, int d, int64_t max_len, int64_t prefix_len) {

@@ -14,6 +14,9 @@
 //
 // Rounding to fewer bits: the weights only, for the second product (codes times a power are exact in bf16 and fp16 within
 // their range); scores, maxima, sums and O are fp32.
+//
+// Bound by reading the codes once: 6 sequences of up to 49159 keys, 8 heads, 494 MB in 95 us, 5.2 TB/s of the 6.5 that a pure read
+// reaches.  Two steps' loads are in flight a wave; their addresses take one page a half, read a step ahead.
 #pragma once
 #include "attend8.h"
 

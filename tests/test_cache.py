@@ -416,6 +416,13 @@ def test_weights_lengths(new, lens, Hq, Hkv):
     _weights_case(new, lens, Hq, Hkv, 64, HF, 16, 16, len(new) + Hq)
 
 
+@pytest.mark.parametrize("n_q,Hq,Hkv", [(12, 8, 1), (13, 8, 1), (33, 2, 2), (96, 1, 1), (97, 1, 1)])
+@pytest.mark.parametrize("block", [0, 16])
+def test_weights_of_even_batches(n_q, Hq, Hkv, block):
+    """Rows of a sequence about 96, where the kernel changes."""
+    _weights_case([n_q] * 3, [n_q, n_q + 200, 5 * n_q + 1], Hq, Hkv, 64, BF, 16, block, n_q, even=True)
+
+
 def test_weights_of_queries_that_attend_to_nothing():
     _weights_case([9, 4], [20, 4], 4, 2, 64, BF, 16, 0, 1, bad_lse=True)
 

@@ -22,16 +22,16 @@ SIZES = [64, 80, 96, 128]
 PATHS = {
     (1, 1, 4, 4, 16, 1, 0): ([("rows", 16)], False, False),
     (1, 1, 4, 4, 16, 1, 77): ([("rows", 16)], False, True),
-    (1, 1, 4, 4, 16, 50, 0): ([("rows", 16)], True, False),
+    (1, 1, 4, 4, 64, 50, 0): ([("rows", 16)], True, False),
     (64, 3, 28, 4, 16, 1, 0): ([("rows", 32)], False, False),
     (64, 3, 28, 4, 16, 1, 77): ([("rows", 32)], False, True),
-    (8, 3, 28, 4, 64, 50, 0): ([("rows", 32)], True, False),
+    (1, 16, 40, 8, 64, 50, 0): ([("rows", 32)], True, False),
     (64, 5, 28, 4, 16, 1, 0): ([("tiles", 128)], False, False),
-    (1, 40, 40, 8, 16, 512, 0): ([("tiles", 128)], True, False),
-    (2, 40, 40, 8, 16, 24, 2001): ([("both", 16)], True, False),
-    (24, 5, 28, 4, 16, 50, 5000): ([("both", 32)], True, False),
+    (1, 24, 40, 8, 64, 512, 77): ([("tiles", 128)], True, False),
+    (8, 5, 40, 8, 16, 24, 5000): ([("both", 16)], True, False),
+    (8, 40, 28, 4, 16, 24, 5000): ([("both", 32)], True, False),
     (2, 16, 28, 4, 64, 512, 2001): ([("rows", 16), ("tiles", 128)], True, False),
-    (1, 16, 64, 8, 64, 512, 2001): ([("rows", 32), ("tiles", 128)], True, False),
+    (1, 24, 40, 8, 64, 512, 5000): ([("rows", 32), ("tiles", 128)], True, False),
 }
 
 
