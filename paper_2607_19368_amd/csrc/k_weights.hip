@@ -32,7 +32,7 @@ struct WeightArgs {
 
 // ---- few rows: the new tokens of a batch ----
 // A wave takes 64 keys and holds them while it goes through the rows, 16 at a time.  Bound by reading K once: everything that
-// does not wait for the page table goes out in front of it, and the keys all at once.  One token of 6 sequences of up to
+// does not wait for the page table goes out in front of it, and the keys all at once.  Two tokens of 6 sequences of up to
 // 49159 keys, 8 heads in 8 bits (262 MB): 44 us, 6.0 TB/s (16 keys a wave: 71).
 constexpr int WT_KEYS = 64;              // of a wave
 
