@@ -381,7 +381,7 @@ __global__ __launch_bounds__(256, 2) void k_weights_tiles(WeightArgs a) {
   auto lse_at = [&] { return lse0 + (at <= last ? (int64_t)at_tok * a.Hq + at_head : 0); };
   // lse times log2(e), and how many keys a row sees (0: it gives nothing); limits do not fall from row to row
   auto row_out = [&](int buf, float lse) {
-    const int sees = at >= rows.y || lse == -INFINITY ? 0 : t.n - t.nq + at_tok + 1;
+    const int sees = at >= rows.y || lse == -INFINITY ? 0 : max(0, t.n - t.nq + at_tok + 1);
     const int to = buf * WT_ROWS + 64 * (wave & 1) + lane;
     s_lse[to] = lse * 1.44269504f;
     s_limit[to] = sees;
