@@ -156,7 +156,7 @@ __global__ __launch_bounds__(WPU < 4 ? 256 : 64 * WPU) void k_append8(Append8Arg
   old = min(old, 254);
   const int byte = max(min(max(c8_byte(top), C8_LEAST), MOST), old);
   const float limit = byte == MOST ? C8_TOP_LAST : C8_TOP;
-  const float down = c8_two(254 - byte);
+  const float down = byte == 254 ? 0x1p-127f : c8_two(254 - byte);
 #pragma unroll
   for (int i = 0; i < IT; ++i) {
     const int r = 16 * strip + i * RPI + lane / LPR;

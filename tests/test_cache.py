@@ -340,7 +340,7 @@ def test_paged_values_that_a_row_does_not_see(dt, d):
 
 
 # ---------------------------------------------------------------- weights
-def _weights_case(new, lens, Hq, Hkv, d, dt, page, block, seed, even=False, scale=None, bad_lse=False):
+def _weights_case(new, lens, Hq, Hkv, d, dt, page, block, seed, even=False, scale=None, bad_lse=False, elsewhere=False):
     """Queries that are parts of wider rows; rows past a length hold NaN."""
     g = _gen(seed)
     B, T = len(new), sum(new)
@@ -373,6 +373,8 @@ def _weights_case(new, lens, Hq, Hkv, d, dt, page, block, seed, even=False, scal
                 if lim > 0:
                     s = _rows(k, table[b], lens[b])[:lim, h // (Hq // Hkv)] @ q[rows][i, h].double() * scale
                     lse[rows.start + i, h] = torch.logsumexp(s, 0) + 0.3          # as behind a prefix
+    if elsewhere:                                  # rows that see none of these keys have others
+        lse[lse == -math.inf] = 0.3
     if bad_lse:
         lse[::3] = -math.inf
     w = torch.rand(B, Hkv, table.shape[1] * page, generator=g)
@@ -414,6 +416,29 @@ def test_weights_lengths(new, lens, Hq, Hkv):
     """Queries of one token and of many, in front of which rows lie or not, some that see nothing."""
     _weights_case(new, lens, Hq, Hkv, 64, BF, 16, 0, len(new) + Hq)
     _weights_case(new, lens, Hq, Hkv, 64, HF, 16, 16, len(new) + Hq)
+
+
+@pytest.mark.parametrize("new,lens,Hq", [([60], [30], 1), ([64], [1], 1), ([100], [3], 1), ([20], [11], 5), ([300, 200], [100, 0], 3), ([129], [128], 1), ([500], [257], 2)])
+@pytest.mark.parametrize("block", [0, 16])
+def test_weights_of_more_queries_than_rows(new, lens, Hq, block):
+    """The first queries see nothing; tiles that hold such rows beside others."""
+    for elsewhere in (False, True):
+        _weights_case(new, lens, Hq, 1, 64, BF, 16, block, new[0] + Hq, elsewhere=elsewhere)
+
+
+@pytest.mark.parametrize("byte", [253, 254])
+def test_append_beside_rows_of_the_largest_powers(byte):
+    """A block whose earlier row has a power that append itself does not give: it stays, and the codes are its."""
+    kc, vc = (torch.zeros(1, 1, 16, 64, dtype=torch.uint8).view(CP.CODE).cuda() for _ in range(2))
+    ks, vs = (torch.full((1, 1, 1), byte, dtype=torch.uint8).view(CP.SCALE).cuda() for _ in range(2))
+    kc.view(torch.uint8)[0, 0, 0] = 0x38                                        # 1
+    x = (torch.linspace(-1, 1, 64) * 3e38).to(BF)[None, None]
+    P.slh_kv_append_e4m3(x.cuda(), x.cuda(), kc, vc, ks, vs, torch.zeros(1, 1, dtype=torch.int32).cuda(), torch.tensor([2], dtype=torch.int32).cuda())
+    want = (x.double() * 2.0 ** (127 - byte)).float().to(CP.CODE)[0, 0]         # exact in fp32: at most 4, at least 2^-133 of 8 bits
+    for cache, two in ((kc, ks), (vc, vs)):
+        assert CP.bytes_of(two).item() == byte
+        assert torch.equal(cache[0, 0, 1].cpu().view(torch.uint8), want.view(torch.uint8))
+    assert bool((kc.view(torch.uint8)[0, 0, 0] == 0x38).all()) and not bool(kc.view(torch.uint8)[0, 0, 2:].any())
 
 
 @pytest.mark.parametrize("n_q,Hq,Hkv", [(12, 8, 1), (13, 8, 1), (33, 2, 2), (96, 1, 1), (97, 1, 1)])
