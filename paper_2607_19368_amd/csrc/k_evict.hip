@@ -7,13 +7,13 @@
 // their order: of equal weights the first rows.  A block a sequence and head, which reads its weights once: 32 a thread stay
 // in LDS, and only those behind are read in every pass.  A wave holds a run of the rows, so that the list of what stays needs
 // the counts of the waves in front and no more barriers.  Bound by latency where rows are few (8 sequences of 97 rows, 4 heads:
-// 8 us) and by its one compute unit where they are many: 16384 rows 24 us, of which the counts, one LDS atomic a row, and the
+// 8 us) and by its one compute unit where they are many: 16384 rows 22 us, of which the counts, one LDS atomic a row, and the
 // list take most.
 //
 // k_evict_count, k_evict_gather, k_evict_list: the same for few long sequences, several blocks each: counts of a run; from all
 // counts the bin, and a run's rows in it and above; from all runs' rows in the bin the smallest that stays, then a run's
 // rows behind those of the runs in front.  Integers throughout, so that the order in which blocks run does not show.  48
-// sequences and heads of up to 49157 rows: 8 + 10 + 19 us, where one block each takes 71.
+// sequences and heads of up to 49157 rows: 8 + 10 + 18 us, where one block each takes 71.
 //
 // k_evict_move: rows are moved in place, in chunks of 256, a block a chunk.  Row i of the result comes from row
 // kept[i] >= i, so the rows that a chunk overwrites are read by it and by chunks in front of it, no others: a block loads its
@@ -77,6 +77,21 @@ constexpr int EV_LEAST = 2, EV_RUNS = 8, EV_HELD = 16;     // rows of a thread w
 
 constexpr int EM_THREADS = 512, EM_PASS = EM_THREADS / 8, EM_N = 4, EM_ROWS = EM_PASS * EM_N;   // 8 lanes a row
 static_assert(EM_ROWS >= C8_BLOCK_MOST, "a chunk holds whole blocks");
+
+// Of a wave's 64 rows those stay that are `in`, and of the equal ones the first: `need` in all, `equal` before; f(at) for each,
+// at: four bytes times its place behind `done` (fewer than 2^31; 32 bits beside a base that the wave shares).
+template <class F>
+__device__ __forceinline__ void ev_keep(bool in, bool eq, int need, int& done, int& equal, F&& f) {
+  const unsigned long long sure = __ballot(in), same = __ballot(eq);
+  if (__builtin_expect(same != 0, 0)) {
+    const int before = equal + ev_below(same);
+    if (in || (eq && before < need)) f(4u * (uint32_t)(done + ev_below(sure) + min(before, need)));
+    equal += __popcll(same);
+  } else if (in) {
+    f(4u * (uint32_t)(done + min(equal, need) + ev_below(sure)));
+  }
+  done += __popcll(sure);
+}
 
 // What k_evict_move starts from: rows before; of the chunks to be moved how many have started, and which are loaded.
 __device__ __forceinline__ void ev_start(const EvictArgs& a, int64_t at, int n, int i0, int step) {
@@ -168,10 +183,11 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   auto find = [&] { return ev_find(s_hist, s_same, s_found, need); };
   // rows that stay for sure, and those with the smallest weight that stays, of which the first `need` do
   uint32_t least = 0xffffffffu;                    // none: behind all of them
-  auto kind = [&](auto whole, int j, uint32_t k, unsigned long long& same, unsigned long long& sure) __attribute__((always_inline)) {
-    const bool candidate = decltype(whole)::value || is_candidate(j);
-    same = __ballot(candidate && k == least);
-    sure = __ballot(candidate ? k > least : j < n);
+  auto is_sure = [&](auto whole, int j, uint32_t k) __attribute__((always_inline)) {
+    return decltype(whole)::value || is_candidate(j) ? k > least : j < n;
+  };
+  auto is_same = [&](auto whole, int j, uint32_t k) __attribute__((always_inline)) {
+    return (decltype(whole)::value || is_candidate(j)) && k == least;
   };
   clear();
   auto take = [&](int i, uint32_t k) __attribute__((always_inline)) {
@@ -248,9 +264,7 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   if (!short_list) {
     n_sure = 0;
     each([&](auto whole, int j, uint32_t k) {
-      unsigned long long same, sure;
-      kind(whole, j, k, same, sure);
-      n_same += __popcll(same), n_sure += __popcll(sure);
+      n_same += __popcll(__ballot(is_same(whole, j, k))), n_sure += __popcll(__ballot(is_sure(whole, j, k)));
     });
     __syncthreads();
     if (lane == 0) s_same[wave] = n_same, s_sure[wave] = n_sure;
@@ -264,15 +278,11 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_pick(EvictArgs a) {
   // time, a chunk's loads before its stores
   const bool all_held = steps <= LDS || a.w != a.w_out;
   each([&](auto whole, int j, uint32_t k) {
-    unsigned long long same, sure;
-    kind(whole, j, k, same, sure);
-    const int eq = equal + ev_below(same), to = done + ev_below(sure) + min(eq, need);
-    const bool stays = (sure >> lane & 1) || ((same >> lane & 1) && eq < need);
-    equal += __popcll(same), done += __popcll(sure);
-    if (stays) {
-      kept[to] = j;
-      if (all_held) w_out[to] = ev_weight(k);
-    }
+    const bool in = is_sure(whole, j, k), eq = is_same(whole, j, k);
+    ev_keep(in, eq, need, done, equal, [&](uint32_t at) {
+      *(int*)((char*)kept + at) = j;
+      if (all_held) *(float*)((char*)w_out + at) = ev_weight(k);
+    });
   });
   if (!all_held) {
     __threadfence_block();
@@ -483,16 +493,16 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_list(EvictArgs a) {
   } else {
     done = min(r.begin, a.first) + max(0, r.begin - (r.n - a.last));
   }
-  auto kind = [&](auto whole, int j, uint32_t k, unsigned long long& same, unsigned long long& sure) __attribute__((always_inline)) {
-    const bool candidate = decltype(whole)::value || (unsigned)(j - lo) < (unsigned)m;
-    same = __ballot(candidate && k == least);
-    sure = __ballot(candidate ? k > least : j < r.n);
+  auto is_candidate = [&](int j) { return (unsigned)(j - lo) < (unsigned)m; };
+  auto is_sure = [&](auto whole, int j, uint32_t k) __attribute__((always_inline)) {
+    return decltype(whole)::value || is_candidate(j) ? k > least : j < r.n;
+  };
+  auto is_same = [&](auto whole, int j, uint32_t k) __attribute__((always_inline)) {
+    return (decltype(whole)::value || is_candidate(j)) && k == least;
   };
   int n_same = 0, n_sure = 0;
   rows.each(r, lo, m, [&](auto whole, int j, uint32_t k) {
-    unsigned long long same, sure;
-    kind(whole, j, k, same, sure);
-    n_same += __popcll(same), n_sure += __popcll(sure);
+    n_same += __popcll(__ballot(is_same(whole, j, k))), n_sure += __popcll(__ballot(is_sure(whole, j, k)));
   });
   if (lane == 0) s_same[wave] = n_same, s_sure[wave] = n_sure;
   __syncthreads();
@@ -500,11 +510,11 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_list(EvictArgs a) {
   for (int v = 0; v < EV_WAVES; ++v)
     if (v < wave) equal += s_same[v], done += s_sure[v];
   rows.each(r, lo, m, [&](auto whole, int j, uint32_t k) {
-    unsigned long long same, sure;
-    kind(whole, j, k, same, sure);
-    const int eq = equal + ev_below(same), to = done + ev_below(sure) + min(eq, need);
-    if ((sure >> lane & 1) || ((same >> lane & 1) && eq < need)) kept[to] = j, w_out[to] = ev_weight(k);
-    equal += __popcll(same), done += __popcll(sure);
+    const bool in = is_sure(whole, j, k), eq = is_same(whole, j, k);
+    ev_keep(in, eq, need, done, equal, [&](uint32_t at) {
+      *(int*)((char*)kept + at) = j;
+      *(float*)((char*)w_out + at) = ev_weight(k);
+    });
   });
   clear();
 }
