@@ -584,7 +584,8 @@ int slh_attend_paged(const void *q, int64_t q_st, int64_t q_sh, const void *k_ca
  * A cache in 8 bits: k_cache, v_cache [n_pages][H][page_size][d] bytes of e4m3 codes (four exponent and three mantissa bits, no
  * infinities), k_scale, v_scale [n_pages][H][page_size / block] bytes s.  A code stands for code 2^(s - 127), s from 1 to 254.
  * page_size and block: powers of two, 16 <= block <= 256, block <= page_size <= 65536; n_pages H page_size < 2^31; d: 64,
- * 80, 96 or 128; caches aligned to 16 bytes.  Pages belong to one sequence, unless they are only read (a shared prefix).
+ * 80, 96 or 128; caches aligned to 16 bytes.  A page stands once in the table of one sequence, unless it is only read (a shared
+ * prefix).
  */
 
 /*
@@ -659,7 +660,7 @@ int slh_attend_weights(const void *q, int64_t q_st, int64_t q_sh, const void *k_
  * Caches of dtype SLH_BF16, SLH_F16 or SLH_F32 (any d of slh_kv_append, page_size a power of two up to 65536; no scales), or
  * SLH_E4M3, in 8 bits: the blocks of a sequence that is cut get the smallest power of two for the rows they now
  * hold (at least 2^-126), the codes follow, exactly but for those that become subnormal.
- * Rows of pages outside [0, n_pages) are not read or written.  budget >= 1; first + last <= budget;
+ * Rows of pages outside [0, n_pages) are not read (zeros stand for them where they stay) or written.  budget >= 1; first + last <= budget;
  * max_pages page_size < 2^29; 2 B H ceil(budget / 256) ceil(bytes of a row / 128) <= 2^22.  workspace: slh_kv_evict_workspace()
  * bytes, with max_len = max_pages page_size (aligned to 16, contents need no preparation), which no other call may use until this one has run.
  */

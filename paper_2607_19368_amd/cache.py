@@ -171,7 +171,8 @@ def slh_attend_weights(q, k_cache, page_table, lens, lse, weights, cu_q=None, k_
 
 
 def slh_kv_evict_workspace(B_, H, d, dtype, budget, max_len):
-    """Bytes that slh_kv_evict needs as workspace, for caches of the torch type `dtype` and tables of max_len rows a sequence."""
+    """Bytes that slh_kv_evict needs as workspace on the current device, for caches of the torch type `dtype` and tables of
+    max_len rows a sequence."""
     return int(B.load().slh_kv_evict_workspace(B_, H, d, B.SLH_E4M3 if dtype is _CODE else _DTYPES[dtype], budget, max_len))
 
 
@@ -209,9 +210,7 @@ def slh_kv_evict(k_cache, v_cache, weights, page_table, lens, budget, first=0, l
     wo = _plain("weights_out", weights_out, torch.float32, dev, shape)
     lo = _plain("lens_out", lens_out, torch.int32, dev, (n,))
     kp = _plain("kept", kept, torch.int32, dev, (n, H, budget))
-    need = int(B.load().slh_kv_evict_workspace(n, H, d, code, budget, most * page))
-    if need < 0:
-        raise SLHError("slh_kv_evict: a size that the library does not take")
+    need = _bytes("slh_kv_evict_workspace", dev, (n, H, d, code, budget, most * page))
     workspace, ws = _workspace(need, dev, workspace, k_cache.device, stream)
     _call("slh_kv_evict", dev, stream,
           (*held, code, total, page, block, n, H, d, pages, ld, most, ln, lo, w, wo, budget, first, last, kp, ws, need))
