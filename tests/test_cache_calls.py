@@ -312,6 +312,46 @@ def test_rows_past_32_bits():
 
 
 @gpu
+@pytest.mark.parametrize("n", [17001, 40000])
+def test_a_graph_of_an_eviction_by_several_blocks(n):
+    """Long sequences: captured, replayed over restored inputs with eager calls between, lengths that change."""
+    B_, H, d, page, budget = 3, 2, 64, 64, 900
+    width = -(-n // page)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    first = {"kc": torch.randn(B_ * width, H, page, d, generator=g, device="cuda").to(BF), "w": torch.rand(B_, H, width * page, generator=g, device="cuda"),
+             "lens": torch.tensor([n, 950, n - 5000], dtype=torch.int32, device="cuda")}
+    first["vc"] = first["kc"].flip(0).contiguous()
+    table = torch.randperm(B_ * width, generator=g, device="cuda").int().view(B_, width)
+    held = {x: t.clone() for x, t in first.items()}
+    kept = torch.empty(B_, H, budget, dtype=torch.int32, device="cuda")
+    ws = torch.empty(P.slh_kv_evict_workspace(B_, H, d, BF, budget, width * page), dtype=torch.uint8, device="cuda")
+
+    def run(s):
+        P.slh_kv_evict(s["kc"], s["vc"], s["w"], table, s["lens"], budget, 4, 64, weights_out=s["w"], lens_out=s["lens"], kept=kept, workspace=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run(held)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(held)
+    for lens in ([n, 950, n - 5000], [899, n, 12000], [n, n, n], [0, 1, n // 2]):
+        first["lens"].copy_(torch.tensor(lens, dtype=torch.int32))
+        eager = {x: t.clone() for x, t in first.items()}
+        run(eager)
+        want = kept.clone()
+        for x, t in first.items():
+            held[x].copy_(t)
+        kept.fill_(-7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(kept, want) and all(torch.equal(held[x], eager[x]) for x in first), lens
+
+
+@gpu
 def test_weights_where_tiles_pass_31_bits():
     """A table for 2^29 rows and 140000 queries: the bound of the tiles is past 31 bits, whatever the lengths."""
     page, most, d, n, T = 65536, 8190, 64, 300, 140000
