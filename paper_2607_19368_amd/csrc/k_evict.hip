@@ -595,8 +595,9 @@ __global__ __launch_bounds__(EM_THREADS) void k_evict_move(EvictArgs a) {
         for (int e = 0; e < 4; ++e)
           for (int s = 0; s < 32; s += 8) most = max(most, (c[e] >> s & 0x7fu) == 0x7fu ? 0u : c[e] >> s & 0x7fu);
       }
-      // maxima of eight rows each
-      const uint32_t top = c8_wave_max(__float_as_uint(__builtin_amdgcn_cvt_pk_f32_fp8(most, false)[0] * c8_two(byte[p])));
+      // Maxima of eight rows each, of code 2^byte by its bits with 2^127 more than a value's, which pass neither end of 32 bits
+      // (exponents up to 135 + 254) as values would that of fp32.
+      const uint32_t top = c8_wave_max(most ? __float_as_uint(__builtin_amdgcn_cvt_pk_f32_fp8(most, false)[0]) + ((uint32_t)byte[p] << 23) : 0u);
       if ((tid & 63) == 0) s_top[p][tid >> 6] = top;
     }
   }
@@ -629,7 +630,7 @@ __global__ __launch_bounds__(EM_THREADS) void k_evict_move(EvictArgs a) {
       uint32_t most = 0;
       for (int e = (g8 >> lg) << lg; e < ((g8 >> lg) + 1) << lg; ++e) most = max(most, all[e]);
       if (to[p] < 0) continue;
-      const int now = min(max(c8_byte(most), C8_LEAST), 254);
+      const int now = min(max(c8_byte(most) - 127, C8_LEAST), 254);
       const float by = c8_two(127 + min(max(byte[p] - now, -126), 127));
       uint4 y = v[p];
       if (byte[p] != now) y = make_uint4(c8_rescaled(y.x, by), c8_rescaled(y.y, by), c8_rescaled(y.z, by), c8_rescaled(y.w, by));
