@@ -128,6 +128,13 @@ __device__ __forceinline__ void at_products_done(T (&x)[N]) {
 // is 2^-24, would otherwise be lost below 2^-25 of the maximum, however many there are.
 constexpr float AT_LAG = 8.f;
 
+// Weights are 2^(s c - mu), mu the maximum times c, rounded: an error of 2^-24 mu that a row's weights share and the division
+// takes out, unless it takes them past what holds them (fp16 from mu = 2^24 on, fp32 from 2^30).  Where a maximum of
+// the wave times c is beyond AT_FAR, or c beyond 1 (products with the largest scores are past fp32), the maximum leaves the scores
+// first.
+constexpr float AT_FAR = 0x1p20f;
+__device__ __forceinline__ bool at_far(float m, float c) { return __ballot(m != -INFINITY && fabsf(m) * c > AT_FAR) != 0; }
+
 // A row that sees no key has the result 0 and no sums, which its limit says and not the sums: keys that it sees may all
 // have the score -inf, and their 0 / 0 is to show.
 constexpr float AT_NO_KEY = -1.f;

@@ -227,6 +227,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[b][e] = 0.f;
   float m = -INFINITY, l = 0.f;                    // m: what the weights are relative to
+  bool far = a.c > 1.f;                            // m leaves the scores first (at_far)
 
   // V^T: lane's element of a 32 x 16 block: row d = lane & 31, keys 4 half + 0..3 and 8 + those
   const int i16 = lane & 15, hi = (lane >> 4) & 1;
@@ -312,6 +313,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
       const float mn = fmaxf(m, top);
       const float keep = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.c);   // of zeros
       m = mn;
+      far |= at_far(m, a.c);
       l *= keep;
 #pragma unroll
       for (int b = 0; b < DB; ++b)
@@ -320,8 +322,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uin
     }
     const float at = m == -INFINITY ? 0.f : m;     // a row that has seen no key yet
     float mu = __builtin_fmaf(at, a.c, -TY::LIFT);
-    if (a.c > 1.f) {
-      // the largest scores times c are past fp32: the maximum leaves them first
+    if (far) {
 #pragma unroll
       for (int kb = 0; kb < NB; ++kb)
 #pragma unroll

@@ -127,6 +127,7 @@ __device__ __forceinline__ void rows8(const Attend8Args& A, int block, float* sm
     }
   }
   at_f32x4 o[NR][DB];
+  bool far = a.c > 1.f;                            // maxima leave the scores first (at_far)
   float m[NR], l[NR];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
@@ -186,6 +187,7 @@ __device__ __forceinline__ void rows8(const Attend8Args& A, int block, float* sm
         const float mn = fmaxf(m[n], top);
         const float keep = m[n] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[n] - mn) * a.c);   // of zeros
         m[n] = mn;
+        far |= at_far(mn, a.c);
         l[n] *= keep;
 #pragma unroll
         for (int b = 0; b < DB; ++b)
@@ -194,8 +196,7 @@ __device__ __forceinline__ void rows8(const Attend8Args& A, int block, float* sm
       }
       const float at = m[n] == -INFINITY ? 0.f : m[n];       // a row that has seen no key yet
       float mu = __builtin_fmaf(at, a.c, -TY::LIFT);
-      if (a.c > 1.f) {
-        // the largest scores times c are past fp32: the maximum leaves them first
+      if (far) {
 #pragma unroll
         for (int f = 0; f < 2; ++f)
 #pragma unroll
