@@ -30,6 +30,16 @@ struct WeightArgs {
   float* part;             // [runs][2][Hkv][256]
 };
 
+// exp(scale s - lse) is 2^(s c - l) with c = scale log2(e) and l = lse log2(e), each rounded once: an error of 2^-23 |lse| or so in the
+// exponent, 2^-11 at WT_FAR.  From there on (past 1 at 2^23, and with an l that may be infinite) the scaled score is
+// rounded as the attention rounds its maximum's for the lse, so that a key that has all of a query's weight gets 1.
+constexpr float WT_FAR = 4096.f;
+__device__ __forceinline__ bool weight_is_far(float lse) { return fabsf(lse) >= WT_FAR && lse != -INFINITY; }
+__device__ __forceinline__ float weight_far(float s, float scale, float lse) {
+#pragma clang fp contract(off)
+  return __builtin_amdgcn_exp2f((s * scale - lse) * 1.44269504f);
+}
+
 // ---- few rows: the new tokens of a batch ----
 // A wave takes 64 keys and holds them while it goes through the rows, 16 at a time.  Bound by reading K once: everything that
 // does not wait for the page table goes out in front of it, and the keys all at once.  Two tokens of 6 sequences of up to
@@ -119,7 +129,7 @@ __global__ __launch_bounds__(256) void k_weights(WeightArgs a) {
 #pragma unroll
   for (int t = 0; t < KT; ++t) sum[t] = 0.f;
   const float c = a.scale * 1.44269504f;
-  auto work = [&]() __attribute__((always_inline)) {
+  auto work_by = [&](auto far) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
       at_f32x4 sc[1] = {at_f32x4{0.f, 0.f, 0.f, 0.f}};
@@ -141,17 +151,36 @@ __global__ __launch_bounds__(256) void k_weights(WeightArgs a) {
       float part = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[0][e], c, -lse[e] * 1.44269504f));
+        const float p = decltype(far)::value ? weight_far(sc[0][e], a.scale, lse[e])
+                                             : __builtin_amdgcn_exp2f(__builtin_fmaf(sc[0][e], c, -lse[e] * 1.44269504f));
         // a row without an lse has no weights to give
         part += key0 + 16 * t + r16 < limit[e] && lse[e] != -INFINITY ? p : 0.f;
       }
       sum[t] += part;
     }
   };
-  work();
+  // Whether an lse is far is asked for at the end, and the rows are gone through again: a branch in front of the products would
+  // wait for the lse (56 rows of 8 x 32768 keys 68 instead of 64 us).
+  bool far = false;
+  auto look = [&] {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) far |= weight_is_far(lse[e]);
+  };
+  const int r_first = r0;
+  work_by(std::false_type{});
+  look();
   while ((r0 += 16) < rows) {
     rows_of();
-    work();
+    work_by(std::false_type{});
+    look();
+  }
+  if (__builtin_expect(__ballot(far) != 0, 0)) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t) sum[t] = 0.f;
+    for (r0 = r_first; r0 < rows; r0 += 16) {
+      rows_of();
+      work_by(std::true_type{});
+    }
   }
 #pragma unroll
   for (int t = 0; t < KT; ++t) {
@@ -286,13 +315,14 @@ __global__ __launch_bounds__(256, 2) void k_weights_tiles(WeightArgs a) {
   constexpr int CH = D / 8, KS = D / 16;
   constexpr int LDX = (WT_ROWS * CH / 64 + 3) / 4;              // 1 KB loads of a tile by a wave
   // One array: of several, the compiler takes every read for one of what loads to LDS write, and waits for them.
-  // Of two tiles: the queries, the lse as they are and times log2(e), the limits, and the ends of each 64 limits.
+  // Of two tiles: the queries, the lse as they are and times log2(e), the limits, the ends of each 64 limits, and whether an lse is far.
   constexpr int TILE = WT_ROWS * D;
-  __shared__ __attribute__((aligned(16))) uint16_t smem[2 * TILE + 12 * WT_ROWS + 16];
+  __shared__ __attribute__((aligned(16))) uint16_t smem[2 * TILE + 12 * WT_ROWS + 20];
   float* const s_raw = (float*)(smem + 2 * TILE);
   float* const s_lse = s_raw + 2 * WT_ROWS;
   int* const s_limit = (int*)s_lse + 2 * WT_ROWS;
   int* const s_ends = s_limit + 2 * WT_ROWS;     // two least limits, two largest
+  int* const s_far = s_ends + 8;                 // whether waves 2 and 3 have met a far lse
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.Hkv, run = blockIdx.x / a.Hkv;
@@ -300,6 +330,7 @@ __global__ __launch_bounds__(256, 2) void k_weights_tiles(WeightArgs a) {
   if (!weight_place(a, run, at_run)) return;
   int64_t left = min(at_run.each, at_run.all - run * at_run.each);
   const float c = a.scale * 1.44269504f;
+  if (wave >= 2) s_far[wave & 1] = 0;
   for (bool begin = true;; begin = false) {
     // the run's tiles of this block of keys
   const WeightSeq& t = at_run.s;
@@ -379,13 +410,18 @@ __global__ __launch_bounds__(256, 2) void k_weights_tiles(WeightArgs a) {
   };
   const float* const lse0 = a.lse + (int64_t)t.q0 * a.Hq + kvh * a.g;
   auto lse_at = [&] { return lse0 + (at <= last ? (int64_t)at_tok * a.Hq + at_head : 0); };
-  // lse times log2(e), and how many keys a row sees (0: it gives nothing); limits do not fall from row to row
+  // lse times log2(e), and how many keys a row sees (0: it gives nothing, or its lse is far: these rows' turn comes behind the
+  // tiles); limits do not fall from row to row
   auto row_out = [&](int buf, float lse) {
-    const int sees = at >= rows.y || lse == -INFINITY ? 0 : max(0, t.n - t.nq + at_tok + 1);
+    const int sees = at >= rows.y || fabsf(lse) >= WT_FAR ? 0 : max(0, t.n - t.nq + at_tok + 1);
     const int to = buf * WT_ROWS + 64 * (wave & 1) + lane;
     s_lse[to] = lse * 1.44269504f;
     s_limit[to] = sees;
-    const int least = __ballot(sees == 0) ? 0 : __builtin_amdgcn_readfirstlane(sees), most = (int)c8_wave_max(sees);
+    int least = __builtin_amdgcn_readfirstlane(sees), most = (int)c8_wave_max(sees);
+    if (__ballot(sees == 0)) {
+      least = 0;
+      if (__ballot(weight_is_far(lse))) s_far[wave & 1] = 1;
+    }
     if (lane == 0) s_ends[4 * buf + (wave & 1)] = least, s_ends[4 * buf + 2 + (wave & 1)] = most;
   };
   // the loads of a tile, and of the lse of the next
@@ -479,6 +515,37 @@ __global__ __launch_bounds__(256, 2) void k_weights_tiles(WeightArgs a) {
       work(std::false_type{}, tile & 1);
     else
       work(std::true_type{}, tile & 1);
+  }
+  // Rows whose lse is far, rare and without haste: 32 rows at a time, of which the others give nothing.  In the tiles' loop this would
+  // take registers from it (1 to 5 % of the time).
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(s_far[0] | s_far[1]), 0) && key0 < t.n) {
+    int l32 = lane & 31, hf = half, q0 = t.q0, end = rows.y;
+    asm volatile("" : "+v"(l32), "+v"(hf), "+s"(q0), "+s"(end));      // what follows from them is made here, and not held throughout
+#pragma unroll 1
+    for (int r0 = rows.x; r0 < end; r0 += 32) {
+      const int row = min(r0 + l32, end - 1), i = row / a.g;
+      const uint16_t* const qp = a.q + (q0 + i) * a.q_st + ((int64_t)kvh * a.g + row - i * a.g) * a.q_sh + 8 * hf;
+      at_f32x16 sc[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[k][e] = 0.f;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const at_u32x4 qf = *(const at_u32x4*)(qp + 16 * s);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sc[k] = TY::mfma(qf, kf[k][s], sc[k]);
+      }
+      at_products_done(sc);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int r = r0 + 4 * hf + 8 * (x / 4) + x % 4, at_r = min(r, end - 1), tok = at_r / a.g;
+        const float l = a.lse[((int64_t)q0 + tok) * a.Hq + kvh * a.g + at_r - tok * a.g];
+        const int sees = r < end && weight_is_far(l) ? t.n - t.nq + tok + 1 : 0;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sum[k] += key0 + 32 * k + l32 < sees ? weight_far(sc[k][x], a.scale, l) : 0.f;
+      }
+    }
   }
 #pragma unroll
   for (int k = 0; k < 2; ++k) {

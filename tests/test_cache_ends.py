@@ -1,5 +1,7 @@
 """The operators of a smaller cache at the ends of what their contracts allow: powers of two that only a cache from elsewhere
-holds."""
+holds, scores far from zero."""
+import math
+
 import pytest
 import torch
 
@@ -7,6 +9,7 @@ import cache_plain as CP
 import paper_2607_19368_amd as P
 
 gpu = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
 
 
 def _gen(seed):
@@ -50,3 +53,87 @@ def test_evict_powers_of_both_ends(d, page, block, powers):
                 nan = torch.isnan(y)
                 assert torch.equal(torch.isnan(have.float()), nan), (h, i0)
                 assert torch.equal(have.view(torch.uint8)[~nan], want.view(torch.uint8)[~nan]), (h, i0)
+
+
+# ---------------------------------------------------------------- weights
+def _far_case(d, dt, block, n, n_q, Hq, at, big_q, big_k, seed):
+    """A cache of one sequence whose key `at` is (big_k, 0, ...), and queries (big_q u_i, ...) with u_i in eight bits."""
+    g = _gen(seed)
+    page = 32
+    width = -(-n // page)
+    x = torch.randn(width, 1, page, d, generator=g).clamp(-4, 4)
+    x[at // page, 0, at % page] = 0
+    x[at // page, 0, at % page, 0] = big_k
+    q = torch.randn(1, n_q, Hq, d, generator=g).to(dt)
+    u = 1 - (torch.arange(n_q * Hq).view(n_q, Hq) % 100) / 256
+    q[0, :, :, 0] = (big_q * u).to(dt)
+    assert bool((q[0, :, :, 0].double() == big_q * u.double()).all())
+    if block:
+        kc, ks = CP.held(x, block)
+        k16 = None
+        assert float(CP.values(kc, ks)[at // page, 0, at % page, 0]) == big_k
+    else:
+        kc, ks = x.to(dt), None
+    return q.cuda(), kc.cuda(), None if ks is None else ks.cuda(), torch.arange(width, dtype=torch.int32).cuda()[None], torch.tensor([n], dtype=torch.int32).cuda(), u
+
+
+@gpu
+@pytest.mark.parametrize("dt,big_q,big_k,scale", [(BF, 2.0 ** 60, 1.5 * 2.0 ** 60, 128.0), (BF, 2.0 ** 60, 1.5 * 2.0 ** 60, 0.3), (BF, 2.0 ** 20, 1.5 * 2.0 ** 14, 0.3),
+                                                  (BF, 2.0 ** 20, 2.0 ** 20, 1e26), (HF, 2.0 ** 14, 1.5 * 2.0 ** 14, 37.7), (HF, 2.0 ** 10, 1.75 * 2.0 ** 13, 0.7)])
+@pytest.mark.parametrize("block", [0, 16])
+@pytest.mark.parametrize("d,n_q", [(64, 2), (80, 3), (96, 130), (128, 2), (128, 150)])
+def test_weights_of_a_key_that_takes_all(dt, big_q, big_k, scale, block, d, n_q):
+    """Scores up to fp32's end, whatever the scale: the key that has all of a query's weight gets 1 from it, the others nothing."""
+    n, Hq, at = 300, 2, 77
+    q, kc, ks, table, lens, u = _far_case(d, dt, block, n, n_q, Hq, at, big_q, big_k, d + n_q)
+    lse = torch.empty(1, n_q, Hq, device="cuda")
+    if block:
+        P.slh_attend_paged_e4m3(q, kc, torch.zeros_like(kc.view(torch.uint8)).view(CP.CODE), ks, ks, table, lens, scale=scale, lse_out=lse)
+    else:
+        P.slh_attend_paged(q, kc, torch.zeros_like(kc), table, lens, scale=scale, lse_out=lse)
+    # one product, exact in fp32, times the scale in fp32
+    s = (big_q * big_k * u.double()).float()
+    assert torch.equal(lse[0].cpu(), s * torch.tensor(scale, dtype=torch.float32))
+    w = torch.zeros(1, 1, table.shape[1] * 32, device="cuda")
+    P.slh_attend_weights(q, kc, table, lens, lse, w, k_scale=ks, scale=scale)
+    want = torch.zeros(w.shape)
+    want[0, 0, at] = n_q * Hq
+    assert torch.equal(w.cpu(), want)
+
+
+@gpu
+@pytest.mark.parametrize("scale", [1.0, 8.0, 2.0 ** -60])
+@pytest.mark.parametrize("block", [0, 16])
+@pytest.mark.parametrize("d,n_q", [(64, 2), (128, 17), (80, 140)])
+def test_weights_of_large_and_ordinary_scores(scale, block, d, n_q):
+    """Scores of 2560 and of 6400 in turn, by row: each within what fp32 holds of them; queries with an lse of either infinity give nothing."""
+    g = _gen(n_q)
+    n, Hq, page = 400, 2, 16
+    x = torch.randn(n // page, 1, page, d, generator=g)
+    x[..., 0] = 64
+    if block:
+        kc, ks = CP.held(x, block)
+        k = CP.values(kc, ks)
+    else:
+        kc, ks = x.to(BF), None
+        k = kc.double()
+    k = k.transpose(1, 2).flatten(0, 1)
+    q = torch.randn(n_q, Hq, d, generator=g)
+    q[:, :, 0] = torch.where(torch.arange(n_q * Hq).view(n_q, Hq) % 3 == 0, 100, 40)
+    q = (q / scale ** 0.5).to(BF)
+    if scale == 2.0 ** -60:
+        q = q * 2.0 ** 30
+    s = torch.einsum("ihd,nd->ihn", q.double(), k[:, 0]) * scale
+    limit = torch.arange(n_q) + n - n_q + 1
+    s = s.masked_fill(torch.arange(n) >= limit[:, None, None], -math.inf)
+    lse = torch.logsumexp(s, -1).float()
+    lse[1::7] = -math.inf
+    lse[0, 1] = math.inf
+    w = torch.zeros(1, 1, n, device="cuda")
+    P.slh_attend_weights(q[None].cuda(), kc.cuda(), torch.arange(n // page, dtype=torch.int32).cuda()[None], torch.tensor([n], dtype=torch.int32).cuda(),
+                         lse[None].cuda(), w, k_scale=None if ks is None else ks.cuda(), scale=scale)
+    gives = torch.where(torch.isinf(lse), torch.tensor(-math.inf), lse)
+    want, tol = CP.weights(q, k, gives, limit, scale)
+    tol += n_q * Hq * 2.0 ** -126                  # terms below the smallest normal number may be zeros
+    assert bool(((w[0].double().cpu() - want).abs() <= tol).all()), float(((w[0].double().cpu() - want).abs() - tol).max())
+    assert float(want.max()) > 0
