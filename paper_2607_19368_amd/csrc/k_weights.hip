@@ -5,7 +5,7 @@
 // same bits every run.  S (rows x keys) = Q K^T, so that a lane holds several rows of one key and adds within its
 // registers; the lanes of a key are added at the end.  Everything is fp32.
 #include "attend8.h"
-#include "attend_plan.h"
+#include "weights_plan.h"
 
 namespace slh {
 
@@ -203,18 +203,11 @@ __global__ __launch_bounds__(256) void k_weights(WeightArgs a) {
 // ahead and are read by all four waves.  Bound by the exponentials: for 32 x 32 scores 256 cycles of products beside 16 times (an
 // addition to the product, an exponential, a sum).  Hence the exponent as one operation, log2(e) in the scale and
 // in the lse that is prepared with the rows, and the next products between the exponentials.
-constexpr int WT_ROWS = 128, WT_BLOCK_KEYS = 256;
 
-// Inclusive sums over the lanes of a wave; wide: past 31 bits.
+// Inclusive sums over the lanes of a wave; wide: of numbers below 2^45, past 31 bits in two parts.
 __device__ __forceinline__ int64_t weight_scan(int64_t v, bool wide) {
   if (!wide) return c8_wave_scan((int)v);
-  const int lane = threadIdx.x & 63;
-#pragma unroll 1
-  for (int x = 1; x < 64; x <<= 1) {
-    const int64_t u = __shfl_up((long long)v, x);
-    if (lane >= x) v += u;
-  }
-  return v;
+  return c8_wave_scan((int)(v & 0xffffff)) + ((int64_t)c8_wave_scan((int)(v >> 24)) << 24);
 }
 
 // The value of lane l, for all (and known to be the same in all).
@@ -561,8 +554,10 @@ __global__ __launch_bounds__(256, 2) void k_weights_tiles(WeightArgs a) {
   // on to the next block of keys, or the first of the next sequence that has tiles
   if (++at_run.kb == t.key_blocks) {
     at_run.kb = 0;
-    do at_run.s = weight_seq_of_all(a, ++at_run.b);
-    while (!at_run.s.row_tiles || !at_run.s.key_blocks);
+    do {
+      if (++at_run.b >= a.B) return;               // never, as the counts are exact
+      at_run.s = weight_seq_of_all(a, at_run.b);
+    } while (!at_run.s.row_tiles || !at_run.s.key_blocks);
   }
   at_run.tile = at_run.s.first(a.g, at_run.kb);
   __syncthreads();                                 // every wave is done with the last tile
@@ -600,26 +595,6 @@ static void weights_launch(const WeightArgs& a, bool tiles, int d, int64_t block
     case 96: go(std::integral_constant<int, 96>{}); break;
     default: go(std::integral_constant<int, 128>{}); break;
   }
-}
-
-// Which kernel, and over how many blocks a head's tiles are spread: all that run at once.
-struct WeightPlan {
-  bool tiles;
-  int runs;
-  int64_t bytes;
-};
-//
-// By rows of a sequence.  Few rows and tiles, 4 key/value heads of 7 and 8 of 4: 56 and 64 rows of 8 sequences of 32768 keys
-// 65 and 89, 134 and 177 us; 112 and 128 rows 93 and 89, 201 and 174; 448 and 256 rows 272 and 191, 334 and 233; of 4096
-// keys, 56 and 448 rows: 13 and 21, 49 and 35 us.  Where the sequences' numbers differ, one may have nearly all rows (4000 of 64
-// sequences' 4063 are 63 a sequence), which are far slower by few: tiles from the smaller number on, that loses at most 2.1 times.
-static WeightPlan weights_plan(int64_t Tq, int B, int Hkv, int g, bool even) {
-  WeightPlan p = {};
-  p.tiles = Tq * g > (even ? 96 : 32) * (int64_t)B;
-  if (!p.tiles) return p;
-  p.runs = std::max(1, 2 * attend_cus() / Hkv);
-  p.bytes = p.runs > 1 ? 8 * (int64_t)p.runs * Hkv * WT_BLOCK_KEYS : 0;
-  return p;
 }
 
 static bool weights_sizes_ok(int64_t Tq, int B, int Hq, int Hkv, int d, int64_t max_len) {
@@ -665,7 +640,7 @@ int slh_attend_weights(const void* q, int64_t q_st, int64_t q_sh, const void* k_
   a.lens = lens, a.cu = cu_q, a.B = B, a.n_each = cu_q ? 0 : (int)(Tq / B), a.Hq = Hq, a.Hkv = Hkv, a.g = Hq / Hkv;
   a.Tq = Tq, a.lse = lse, a.scale = (float)scale, a.w = weights;
   a.runs = p.runs, a.part = (float*)workspace;
-  a.wide = (Tq * a.g / WT_ROWS + B) * (a.max_rows / WT_BLOCK_KEYS + 1) + p.runs > INT32_MAX;
+  a.wide = weights_wide(Tq, B, a.g, a.max_rows, !cu_q, p.runs);
   a.key_blocks = (a.max_rows + 4 * WT_KEYS - 1) / (4 * WT_KEYS);
   const int64_t blocks = (p.tiles ? p.runs : (int64_t)B * a.key_blocks) * Hkv;
   (void)hipGetLastError();

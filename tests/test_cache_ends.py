@@ -1,12 +1,16 @@
 """The operators of a smaller cache at the ends of what their contracts allow: powers of two that only a cache from elsewhere
 holds, scores far from zero."""
+import ctypes
 import math
+import os
+import subprocess
 
 import pytest
 import torch
 
 import cache_plain as CP
 import paper_2607_19368_amd as P
+from paper_2607_19368_amd import build as BUILD
 
 gpu = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -137,3 +141,53 @@ def test_weights_of_large_and_ordinary_scores(scale, block, d, n_q):
     tol += n_q * Hq * 2.0 ** -126                  # terms below the smallest normal number may be zeros
     assert bool(((w[0].double().cpu() - want).abs() <= tol).all()), float(((w[0].double().cpu() - want).abs() - tol).max())
     assert float(want.max()) > 0
+
+
+@pytest.fixture(scope="module")
+def wide(tmp_path_factory):
+    out = os.path.join(str(tmp_path_factory.mktemp("weights")), "libweightsstub.so")
+    cmd = [BUILD.HIPCC, "--offload-host-only", "-x", "hip", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wl,-Bsymbolic", "-w",
+           "-I", os.path.join(BUILD.ROOT, "include"), "-I", BUILD.CSRC, os.path.join(BUILD.ROOT, "tests", "weights_stub.cpp"), "-o", out]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    f = ctypes.CDLL(out).stub_weights_wide
+    f.argtypes = [ctypes.c_int64] + 5 * [ctypes.c_int]
+    return f
+
+
+def test_tiles_of_any_cu_are_counted_in_bits_that_hold_them(wide):
+    """cu_q lies in device memory: entries that do not ascend may give every other sequence all queries."""
+    for B, Tq, g, rows, in ((1 << 16, 16384, 8, 16384), (64, 1 << 20, 8, 131072), (2, 1 << 27, 8, 1 << 16), (1, 140000, 1, 8190 * 65536), (23, 12007, 4, 1472),
+                            (3, 192, 5, 9216), (1 << 20, 1 << 20, 1, 256), (4096, 4096, 7, 65536), (1024, 65536, 8, 131072), (1023, 65536, 8, 131072)):
+        key_blocks = -(-rows // 256)
+        most = B * -(-Tq * g // 128) * key_blocks
+        assert wide(Tq, B, g, rows, 0, 64) == (most + 64 >= 1 << 31), (B, Tq, g, rows)
+        if Tq % B == 0:
+            assert wide(Tq, B, g, rows, 1, 64) == (B * -(-Tq // B * g // 128) * key_blocks + 64 >= 1 << 31), (B, Tq, g, rows)
+
+
+@gpu
+@pytest.mark.parametrize("block", [0, 16])
+def test_weights_of_entries_that_do_not_ascend(block):
+    """Sequences that share their queries, or have none: each as by itself."""
+    g = _gen(8)
+    page, d, T, Hq = 32, 64, 300, 2
+    bounds = [0, 300, 0, 150, 100, 300, -7, 400, 20]
+    lens = [300, 40, 513, 77, 200, 9, 1024, 33]
+    n, width = len(lens), 32
+    x = torch.randn(n * width, 1, page, d, generator=g)
+    kc, ks = CP.held(x, block) if block else (x.to(BF), None)
+    kc, ks = kc.cuda(), None if ks is None else ks.cuda()
+    table = torch.randperm(n * width, generator=g).int().view(n, width).cuda()
+    q = torch.randn(T, Hq, d, generator=g).to(BF).cuda()
+    lse = torch.full((T, Hq), 6.0, device="cuda")
+    w = torch.zeros(n, 1, width * page, device="cuda")
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    P.slh_attend_weights(q, kc, table, ints(lens), lse, w, cu_q=ints(bounds), k_scale=ks)
+    for b in range(n):
+        lo, hi = (min(max(v, 0), T) for v in bounds[b:b + 2])
+        one = torch.zeros(1, 1, width * page, device="cuda")
+        if lo < hi:
+            P.slh_attend_weights(q[lo:hi].contiguous(), kc, table[b:b + 1], ints(lens[b:b + 1]), lse[lo:hi].contiguous(), one, cu_q=ints([0, hi - lo]), k_scale=ks)
+        # the same positive terms, in another order
+        assert bool(((w[b] - one[0]).abs() <= 2 * T * Hq * 2.0 ** -24 * one[0]).all()), b
