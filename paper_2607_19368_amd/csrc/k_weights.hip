@@ -326,241 +326,241 @@ __global__ __launch_bounds__(256, 2) void k_weights_tiles(WeightArgs a) {
   if (wave >= 2) s_far[wave & 1] = 0;
   for (bool begin = true;; begin = false) {
     // the run's tiles of this block of keys
-  const WeightSeq& t = at_run.s;
-  const int n_tiles = (int)min(left, (int64_t)(t.row_tiles - at_run.tile));
-  const bool whole = at_run.tile == t.first(a.g, at_run.kb) && at_run.tile + n_tiles == t.row_tiles;
-  const int2 rows = make_int2(at_run.tile * WT_ROWS, min(t.nq * a.g, (at_run.tile + n_tiles) * WT_ROWS));
-  const int block0 = at_run.kb * WT_BLOCK_KEYS, key0 = block0 + 64 * wave;
+    const WeightSeq& t = at_run.s;
+    const int n_tiles = (int)min(left, (int64_t)(t.row_tiles - at_run.tile));
+    const bool whole = at_run.tile == t.first(a.g, at_run.kb) && at_run.tile + n_tiles == t.row_tiles;
+    const int2 rows = make_int2(at_run.tile * WT_ROWS, min(t.nq * a.g, (at_run.tile + n_tiles) * WT_ROWS));
+    const int block0 = at_run.kb * WT_BLOCK_KEYS, key0 = block0 + 64 * wave;
 
-  // this wave's keys, one of each 32 a lane, in the type of the queries: d 16 s + 8 half
-  at_u32x4 kf[2][KS];
+    // this wave's keys, one of each 32 a lane, in the type of the queries: d 16 s + 8 half
+    at_u32x4 kf[2][KS];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int j = min(key0 + 32 * k + (lane & 31), t.n - 1);
-    const int page = a.pages[at_run.b * a.ld_pages + (j >> a.lg_page)];
-    const int64_t line = (((int64_t)((unsigned)page < (unsigned)a.n_pages ? page : 0) * a.Hkv + kvh) << a.lg_page) +
-                         (j & ((1 << a.lg_page) - 1));
-    if constexpr (E8) {
-      const uint8_t* kp = (const uint8_t*)a.k + line * D + 8 * half;
-      const float two = c8_two(a.k_two[line >> a.lg_block]);
+    for (int k = 0; k < 2; ++k) {
+      const int j = min(key0 + 32 * k + (lane & 31), t.n - 1);
+      const int page = a.pages[at_run.b * a.ld_pages + (j >> a.lg_page)];
+      const int64_t line = (((int64_t)((unsigned)page < (unsigned)a.n_pages ? page : 0) * a.Hkv + kvh) << a.lg_page) +
+                           (j & ((1 << a.lg_page) - 1));
+      if constexpr (E8) {
+        const uint8_t* kp = (const uint8_t*)a.k + line * D + 8 * half;
+        const float two = c8_two(a.k_two[line >> a.lg_block]);
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const at_u32x2 w = *(const at_u32x2*)(kp + 16 * s);
-        kf[k][s] = at_u32x4{c8_pair<TY, false>(w[0], two), c8_pair<TY, true>(w[0], two), c8_pair<TY, false>(w[1], two),
-                            c8_pair<TY, true>(w[1], two)};
+        for (int s = 0; s < KS; ++s) {
+          const at_u32x2 w = *(const at_u32x2*)(kp + 16 * s);
+          kf[k][s] = at_u32x4{c8_pair<TY, false>(w[0], two), c8_pair<TY, true>(w[0], two), c8_pair<TY, false>(w[1], two),
+                              c8_pair<TY, true>(w[1], two)};
+        }
+      } else {
+        const uint16_t* kp = (const uint16_t*)a.k + line * D + 8 * half;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kf[k][s] = *(const at_u32x4*)(kp + 16 * s);
       }
-    } else {
-      const uint16_t* kp = (const uint16_t*)a.k + line * D + 8 * half;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) kf[k][s] = *(const at_u32x4*)(kp + 16 * s);
     }
-  }
 
-  // Loads of a tile: load l of a wave fills 64 chunks of 16 bytes, this lane's at `from`, of row (tok, head) of the current
-  // tile.  Rows past the last, in the last tile, repeat it.
-  const int last = t.nq * a.g - 1, up_tok = WT_ROWS / a.g, up_head = WT_ROWS - up_tok * a.g;
-  const uint16_t* const qbase = a.q + (int64_t)t.q0 * a.q_st + (int64_t)kvh * a.g * a.q_sh;
-  const int64_t up = up_tok * a.q_st + up_head * a.q_sh, wrap = a.q_st - a.g * a.q_sh;
-  const uint16_t* from[LDX];
-  int head[LDX];
-  auto place = [&](int l, int row) {
-    const int n = (l * 4 + wave) * 64 + lane, r = n / CH, i = min(row + r, last) / a.g;
-    head[l] = min(row + r, last) - i * a.g;
-    from[l] = qbase + i * a.q_st + head[l] * a.q_sh + 8 * ((n - r * CH) ^ wt_swz<D>(r));
-  };
+    // Loads of a tile: load l of a wave fills 64 chunks of 16 bytes, this lane's at `from`, of row (tok, head) of the current
+    // tile.  Rows past the last, in the last tile, repeat it.
+    const int last = t.nq * a.g - 1, up_tok = WT_ROWS / a.g, up_head = WT_ROWS - up_tok * a.g;
+    const uint16_t* const qbase = a.q + (int64_t)t.q0 * a.q_st + (int64_t)kvh * a.g * a.q_sh;
+    const int64_t up = up_tok * a.q_st + up_head * a.q_sh, wrap = a.q_st - a.g * a.q_sh;
+    const uint16_t* from[LDX];
+    int head[LDX];
+    auto place = [&](int l, int row) {
+      const int n = (l * 4 + wave) * 64 + lane, r = n / CH, i = min(row + r, last) / a.g;
+      head[l] = min(row + r, last) - i * a.g;
+      from[l] = qbase + i * a.q_st + head[l] * a.q_sh + 8 * ((n - r * CH) ^ wt_swz<D>(r));
+    };
 #pragma unroll
-  for (int l = 0; l < LDX; ++l) place(l, rows.x);
-  auto load = [&](int buf) {
+    for (int l = 0; l < LDX; ++l) place(l, rows.x);
+    auto load = [&](int buf) {
 #pragma unroll
-    for (int l = 0; l < LDX; ++l)
-      if (WT_ROWS * CH / 64 % 4 == 0 || l * 4 + wave < WT_ROWS * CH / 64)
-        __builtin_amdgcn_global_load_lds((at_gptr)from[l], (at_lptr)(smem + buf * TILE + (l * 4 + wave) * 512), 16, 0, 0);
-  };
-  // on to the tile of rows r0..
-  auto move = [&](int r0) {
-    if (r0 + WT_ROWS - 1 > last) {
+      for (int l = 0; l < LDX; ++l)
+        if (WT_ROWS * CH / 64 % 4 == 0 || l * 4 + wave < WT_ROWS * CH / 64)
+          __builtin_amdgcn_global_load_lds((at_gptr)from[l], (at_lptr)(smem + buf * TILE + (l * 4 + wave) * 512), 16, 0, 0);
+    };
+    // on to the tile of rows r0..
+    auto move = [&](int r0) {
+      if (r0 + WT_ROWS - 1 > last) {
 #pragma unroll
-      for (int l = 0; l < LDX; ++l) place(l, r0);
-      return;
-    }
-    if (up_head == 0) {
+        for (int l = 0; l < LDX; ++l) place(l, r0);
+        return;
+      }
+      if (up_head == 0) {
 #pragma unroll
-      for (int l = 0; l < LDX; ++l) from[l] += up;
-      return;
-    }
+        for (int l = 0; l < LDX; ++l) from[l] += up;
+        return;
+      }
 #pragma unroll
-    for (int l = 0; l < LDX; ++l) {
-      from[l] += up, head[l] += up_head;
-      if (head[l] >= a.g) head[l] -= a.g, from[l] += wrap;
-    }
-  };
-  // Rows `lane` of a tile's first and second 64, by waves 0 and 1 (their lse on the way to LDS) and 2 and 3 (which prepare
-  // them a tile later): row `at` is (at_tok, at_head).
-  int at = rows.x + 64 * (wave & 1) + lane, at_tok = at / a.g, at_head = at - at_tok * a.g;
-  auto next = [&] {
-    at += WT_ROWS, at_tok += up_tok, at_head += up_head;
-    if (at_head >= a.g) at_head -= a.g, ++at_tok;
-  };
-  const float* const lse0 = a.lse + (int64_t)t.q0 * a.Hq + kvh * a.g;
-  auto lse_at = [&] { return lse0 + (at <= last ? (int64_t)at_tok * a.Hq + at_head : 0); };
-  // lse times log2(e), and how many keys a row sees (0: it gives nothing, or its lse is far: these rows' turn comes behind the
-  // tiles); limits do not fall from row to row
-  auto row_out = [&](int buf, float lse) {
-    const int sees = at >= rows.y || fabsf(lse) >= WT_FAR ? 0 : max(0, t.n - t.nq + at_tok + 1);
-    const int to = buf * WT_ROWS + 64 * (wave & 1) + lane;
-    s_lse[to] = lse * 1.44269504f;
-    s_limit[to] = sees;
-    int least = __builtin_amdgcn_readfirstlane(sees), most = (int)c8_wave_max(sees);
-    if (__ballot(sees == 0)) {
-      least = 0;
-      if (__ballot(weight_is_far(lse))) s_far[wave & 1] = 1;
-    }
-    if (lane == 0) s_ends[4 * buf + (wave & 1)] = least, s_ends[4 * buf + 2 + (wave & 1)] = most;
-  };
-  // the loads of a tile, and of the lse of the next
-  auto fetch = [&](int tile) {
-    if (tile) move(rows.x + tile * WT_ROWS);
-    load(tile & 1);
-    if (wave < 2) {
-      next();
-      __builtin_amdgcn_global_load_lds((at_gptr)lse_at(), (at_lptr)(s_raw + ((tile + 1) & 1) * WT_ROWS + 64 * wave), 4, 0, 0);
-    }
-  };
+      for (int l = 0; l < LDX; ++l) {
+        from[l] += up, head[l] += up_head;
+        if (head[l] >= a.g) head[l] -= a.g, from[l] += wrap;
+      }
+    };
+    // Rows `lane` of a tile's first and second 64, by waves 0 and 1 (their lse on the way to LDS) and 2 and 3 (which prepare
+    // them a tile later): row `at` is (at_tok, at_head).
+    int at = rows.x + 64 * (wave & 1) + lane, at_tok = at / a.g, at_head = at - at_tok * a.g;
+    auto next = [&] {
+      at += WT_ROWS, at_tok += up_tok, at_head += up_head;
+      if (at_head >= a.g) at_head -= a.g, ++at_tok;
+    };
+    const float* const lse0 = a.lse + (int64_t)t.q0 * a.Hq + kvh * a.g;
+    auto lse_at = [&] { return lse0 + (at <= last ? (int64_t)at_tok * a.Hq + at_head : 0); };
+    // lse times log2(e), and how many keys a row sees (0: it gives nothing, or its lse is far: these rows' turn comes behind the
+    // tiles); limits do not fall from row to row
+    auto row_out = [&](int buf, float lse) {
+      const int sees = at >= rows.y || fabsf(lse) >= WT_FAR ? 0 : max(0, t.n - t.nq + at_tok + 1);
+      const int to = buf * WT_ROWS + 64 * (wave & 1) + lane;
+      s_lse[to] = lse * 1.44269504f;
+      s_limit[to] = sees;
+      int least = __builtin_amdgcn_readfirstlane(sees), most = (int)c8_wave_max(sees);
+      if (__ballot(sees == 0)) {
+        least = 0;
+        if (__ballot(weight_is_far(lse))) s_far[wave & 1] = 1;
+      }
+      if (lane == 0) s_ends[4 * buf + (wave & 1)] = least, s_ends[4 * buf + 2 + (wave & 1)] = most;
+    };
+    // the loads of a tile, and of the lse of the next
+    auto fetch = [&](int tile) {
+      if (tile) move(rows.x + tile * WT_ROWS);
+      load(tile & 1);
+      if (wave < 2) {
+        next();
+        __builtin_amdgcn_global_load_lds((at_gptr)lse_at(), (at_lptr)(s_raw + ((tile + 1) & 1) * WT_ROWS + 64 * wave), 4, 0, 0);
+      }
+    };
 
-  float sum[2] = {0.f, 0.f};
-  const int tiles = (rows.y - rows.x + WT_ROWS - 1) / WT_ROWS;
-  if (wave >= 2) row_out(0, *lse_at());
-  fetch(0);
-  // the keys are waited for here, and not, with every load in flight, in each tile
+    float sum[2] = {0.f, 0.f};
+    const int tiles = (rows.y - rows.x + WT_ROWS - 1) / WT_ROWS;
+    if (wave >= 2) row_out(0, *lse_at());
+    fetch(0);
+    // the keys are waited for here, and not, with every load in flight, in each tile
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(kf[k][s]));
-  // A tile's rows, 32 at a time.  The products of the next 32 go out between the exponentials of these, in an order that is
-  // kept: left to itself the compiler puts them one behind the other, and each waits for the other's unit.
-  auto work = [&](auto masked, int buf) __attribute__((always_inline)) {
-    constexpr int NB = WT_ROWS / 32;
-    const uint16_t* const row = smem + buf * TILE + (lane & 31) * D;
-    const float* const l_at = s_lse + buf * WT_ROWS + 4 * half;
-    const int* const m_at = s_limit + buf * WT_ROWS + 4 * half;
-    at_f32x16 sc[2][2];
-    at_u32x4 qf[2];
-    auto q_read = [&](int rb, int s) { return *(const at_u32x4*)(row + 32 * rb * D + 8 * ((2 * s + half) ^ wt_swz<D>(lane & 31))); };
-    qf[0] = q_read(0, 0);
+      for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(kf[k][s]));
+    // A tile's rows, 32 at a time.  The products of the next 32 go out between the exponentials of these, in an order that is
+    // kept: left to itself the compiler puts them one behind the other, and each waits for the other's unit.
+    auto work = [&](auto masked, int buf) __attribute__((always_inline)) {
+      constexpr int NB = WT_ROWS / 32;
+      const uint16_t* const row = smem + buf * TILE + (lane & 31) * D;
+      const float* const l_at = s_lse + buf * WT_ROWS + 4 * half;
+      const int* const m_at = s_limit + buf * WT_ROWS + 4 * half;
+      at_f32x16 sc[2][2];
+      at_u32x4 qf[2];
+      auto q_read = [&](int rb, int s) { return *(const at_u32x4*)(row + 32 * rb * D + 8 * ((2 * s + half) ^ wt_swz<D>(lane & 31))); };
+      qf[0] = q_read(0, 0);
 #pragma unroll
-    for (int rb = -1; rb < NB; ++rb) {
-      const bool more = rb + 1 < NB;
-      at_f32x16(&nx)[2] = sc[(rb + 1) & 1];
-      at_f32x16(&cu)[2] = sc[rb & 1];
-      float part[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
-      at_f32x4 l4[4];
-      at_u32x4 m4[4];
-      if (rb >= 0) {
+      for (int rb = -1; rb < NB; ++rb) {
+        const bool more = rb + 1 < NB;
+        at_f32x16(&nx)[2] = sc[(rb + 1) & 1];
+        at_f32x16(&cu)[2] = sc[rb & 1];
+        float part[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+        at_f32x4 l4[4];
+        at_u32x4 m4[4];
+        if (rb >= 0) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          l4[q] = *(const at_f32x4*)(l_at + 32 * rb + 8 * q);
-          if (decltype(masked)::value) m4[q] = *(const at_u32x4*)(m_at + 32 * rb + 8 * q);
+          for (int q = 0; q < 4; ++q) {
+            l4[q] = *(const at_f32x4*)(l_at + 32 * rb + 8 * q);
+            if (decltype(masked)::value) m4[q] = *(const at_u32x4*)(m_at + 32 * rb + 8 * q);
+          }
+        }
+        if (more) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) nx[k][e] = 0.f;
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          if (more) {
+            const int n = (rb + 1) * KS + s + 1;           // the next operand, of these rows or the next 32
+            if (n < NB * KS) qf[n & 1] = q_read(n / KS, n % KS);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) nx[k] = TY::mfma(qf[(n - 1) & 1], kf[k][s], nx[k]);
+          }
+          if (rb >= 0) {
+#pragma unroll
+            for (int x = s * 16 / KS; x < (s + 1) * 16 / KS; ++x)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                float add = __builtin_amdgcn_exp2f(__builtin_fmaf(cu[k][x], c, -l4[x / 4][x % 4]));
+                if (decltype(masked)::value) add = key0 + 32 * k + (lane & 31) < (int)m4[x / 4][x % 4] ? add : 0.f;
+                part[k][x & 1] += add;
+              }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sum[k] += part[k][0] + part[k][1];
+      }
+    };
+    for (int tile = 0; tile < tiles; ++tile) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");    // this tile has landed; the other buffer is free
+      if (tile + 1 < tiles) {
+        fetch(tile + 1);
+        if (wave >= 2) {
+          next();
+          row_out((tile + 1) & 1, s_raw[((tile + 1) & 1) * WT_ROWS + 64 * (wave & 1) + lane]);
         }
       }
-      if (more) {
+      if (key0 >= t.n) continue;
+      const at_u32x4 ends = *(const at_u32x4*)(s_ends + 4 * (tile & 1));
+      if (__builtin_amdgcn_readfirstlane(max((int)ends[2], (int)ends[3])) <= key0) continue;   // none sees any
+      if (__builtin_amdgcn_readfirstlane(min((int)ends[0], (int)ends[1])) >= key0 + 64)      // every row of the tile sees all of this wave's keys
+        work(std::false_type{}, tile & 1);
+      else
+        work(std::true_type{}, tile & 1);
+    }
+    // Rows whose lse is far, rare and without haste: 32 rows at a time, of which the others give nothing.  In the tiles' loop this would
+    // take registers from it (1 to 5 % of the time).
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(s_far[0] | s_far[1]), 0) && key0 < t.n) {
+      int l32 = lane & 31, hf = half, q0 = t.q0, end = rows.y;
+      asm volatile("" : "+v"(l32), "+v"(hf), "+s"(q0), "+s"(end));      // what follows from them is made here, and not held throughout
+#pragma unroll 1
+      for (int r0 = rows.x; r0 < end; r0 += 32) {
+        const int row = min(r0 + l32, end - 1), i = row / a.g;
+        const uint16_t* const qp = a.q + (q0 + i) * a.q_st + ((int64_t)kvh * a.g + row - i * a.g) * a.q_sh + 8 * hf;
+        at_f32x16 sc[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) nx[k][e] = 0.f;
-      }
+          for (int e = 0; e < 16; ++e) sc[k][e] = 0.f;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        if (more) {
-          const int n = (rb + 1) * KS + s + 1;           // the next operand, of these rows or the next 32
-          if (n < NB * KS) qf[n & 1] = q_read(n / KS, n % KS);
+        for (int s = 0; s < KS; ++s) {
+          const at_u32x4 qf = *(const at_u32x4*)(qp + 16 * s);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) nx[k] = TY::mfma(qf[(n - 1) & 1], kf[k][s], nx[k]);
+          for (int k = 0; k < 2; ++k) sc[k] = TY::mfma(qf, kf[k][s], sc[k]);
         }
-        if (rb >= 0) {
+        at_products_done(sc);
 #pragma unroll
-          for (int x = s * 16 / KS; x < (s + 1) * 16 / KS; ++x)
+        for (int x = 0; x < 16; ++x) {
+          const int r = r0 + 4 * hf + 8 * (x / 4) + x % 4, at_r = min(r, end - 1), tok = at_r / a.g;
+          const float l = a.lse[((int64_t)q0 + tok) * a.Hq + kvh * a.g + at_r - tok * a.g];
+          const int sees = r < end && weight_is_far(l) ? t.n - t.nq + tok + 1 : 0;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              float add = __builtin_amdgcn_exp2f(__builtin_fmaf(cu[k][x], c, -l4[x / 4][x % 4]));
-              if (decltype(masked)::value) add = key0 + 32 * k + (lane & 31) < (int)m4[x / 4][x % 4] ? add : 0.f;
-              part[k][x & 1] += add;
-            }
+          for (int k = 0; k < 2; ++k) sum[k] += key0 + 32 * k + l32 < sees ? weight_far(sc[k][x], a.scale, l) : 0.f;
         }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k) sum[k] += part[k][0] + part[k][1];
-    }
-  };
-  for (int tile = 0; tile < tiles; ++tile) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");    // this tile has landed; the other buffer is free
-    if (tile + 1 < tiles) {
-      fetch(tile + 1);
-      if (wave >= 2) {
-        next();
-        row_out((tile + 1) & 1, s_raw[((tile + 1) & 1) * WT_ROWS + 64 * (wave & 1) + lane]);
       }
     }
-    if (key0 >= t.n) continue;
-    const at_u32x4 ends = *(const at_u32x4*)(s_ends + 4 * (tile & 1));
-    if (__builtin_amdgcn_readfirstlane(max((int)ends[2], (int)ends[3])) <= key0) continue;   // none sees any
-    if (__builtin_amdgcn_readfirstlane(min((int)ends[0], (int)ends[1])) >= key0 + 64)      // every row of the tile sees all of this wave's keys
-      work(std::false_type{}, tile & 1);
-    else
-      work(std::true_type{}, tile & 1);
-  }
-  // Rows whose lse is far, rare and without haste: 32 rows at a time, of which the others give nothing.  In the tiles' loop this would
-  // take registers from it (1 to 5 % of the time).
-  if (__builtin_expect(__builtin_amdgcn_readfirstlane(s_far[0] | s_far[1]), 0) && key0 < t.n) {
-    int l32 = lane & 31, hf = half, q0 = t.q0, end = rows.y;
-    asm volatile("" : "+v"(l32), "+v"(hf), "+s"(q0), "+s"(end));      // what follows from them is made here, and not held throughout
-#pragma unroll 1
-    for (int r0 = rows.x; r0 < end; r0 += 32) {
-      const int row = min(r0 + l32, end - 1), i = row / a.g;
-      const uint16_t* const qp = a.q + (q0 + i) * a.q_st + ((int64_t)kvh * a.g + row - i * a.g) * a.q_sh + 8 * hf;
-      at_f32x16 sc[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sc[k][e] = 0.f;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const at_u32x4 qf = *(const at_u32x4*)(qp + 16 * s);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) sc[k] = TY::mfma(qf, kf[k][s], sc[k]);
-      }
-      at_products_done(sc);
-#pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const int r = r0 + 4 * hf + 8 * (x / 4) + x % 4, at_r = min(r, end - 1), tok = at_r / a.g;
-        const float l = a.lse[((int64_t)q0 + tok) * a.Hq + kvh * a.g + at_r - tok * a.g];
-        const int sees = r < end && weight_is_far(l) ? t.n - t.nq + tok + 1 : 0;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) sum[k] += key0 + 32 * k + l32 < sees ? weight_far(sc[k][x], a.scale, l) : 0.f;
-      }
+    for (int k = 0; k < 2; ++k) {
+      const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[k]), __float_as_uint(sum[k]), false, false);
+      sum[k] = __uint_as_float(w32[0]) + __uint_as_float(w32[1]);
+      const int j = key0 + 32 * k + (lane & 31);
+      if (half == 0 && whole && j < t.n) a.w[((int64_t)at_run.b * a.Hkv + kvh) * a.max_rows + j] += sum[k];
+      // a block has two such runs at most: one that goes on from the block before, one that the next goes on with
+      if (half == 0 && !whole) a.part[((2 * (int64_t)run + !begin) * a.Hkv + kvh) * WT_BLOCK_KEYS + j - block0] = sum[k];
     }
-  }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[k]), __float_as_uint(sum[k]), false, false);
-    sum[k] = __uint_as_float(w32[0]) + __uint_as_float(w32[1]);
-    const int j = key0 + 32 * k + (lane & 31);
-    if (half == 0 && whole && j < t.n) a.w[((int64_t)at_run.b * a.Hkv + kvh) * a.max_rows + j] += sum[k];
-    // a block has two such runs at most: one that goes on from the block before, one that the next goes on with
-    if (half == 0 && !whole) a.part[((2 * (int64_t)run + !begin) * a.Hkv + kvh) * WT_BLOCK_KEYS + j - block0] = sum[k];
-  }
-  left -= n_tiles;
-  if (left == 0) return;
-  // on to the next block of keys, or the first of the next sequence that has tiles
-  if (++at_run.kb == t.key_blocks) {
-    at_run.kb = 0;
-    do {
-      if (++at_run.b >= a.B) return;               // never, as the counts are exact
-      at_run.s = weight_seq_of_all(a, at_run.b);
-    } while (!at_run.s.row_tiles || !at_run.s.key_blocks);
-  }
-  at_run.tile = at_run.s.first(a.g, at_run.kb);
-  __syncthreads();                                 // every wave is done with the last tile
+    left -= n_tiles;
+    if (left == 0) return;
+    // on to the next block of keys, or the first of the next sequence that has tiles
+    if (++at_run.kb == t.key_blocks) {
+      at_run.kb = 0;
+      do {
+        if (++at_run.b >= a.B) return;               // never, as the counts are exact
+        at_run.s = weight_seq_of_all(a, at_run.b);
+      } while (!at_run.s.row_tiles || !at_run.s.key_blocks);
+    }
+    at_run.tile = at_run.s.first(a.g, at_run.kb);
+    __syncthreads();                                 // every wave is done with the last tile
   }
 }
 
