@@ -65,7 +65,8 @@ template <int D> constexpr int at_lds() { return 4 * at_lds_tile<D>() + 2 * AT_W
 
 // E8: keys and values of a cache in 8 bits.  They wait in registers while the tile before is worked on, and are converted to
 // TY, with their powers of two, on the way to LDS, once for the block's 128 rows.  128 questions of 7 rows a head behind a
-// prefix of 32768 rows: 121 us by blocks of 32 rows, which each convert it anew, 88 in tiles (16-bit rows: 86).
+// prefix of 32768 rows: 121 us by blocks of 32 rows, which each convert it anew, 89 in tiles, as with 16-bit rows (95 and 97 us
+// beside each other on another card).
 template <class TY, int D, bool PAGED, int KW, bool E8 = false>
 __device__ __forceinline__ void attend_tiles(const AttendArgs& a, int block, uint16_t* smem, const AtHeld& held = AtHeld{}) {
   constexpr int CH = D / 8;                        // 16-byte chunks of a row

@@ -12,7 +12,7 @@
 // once.
 //
 // Bound by the latency from cu and lens through the page table to the rows where tokens are few (61 sequences, one token
-// each: 6 us), else by memory: 16384 tokens of 8 heads of 128 (fp16 read, codes written, 109 MB) 30 us, 3.6 TB/s; a
+// each: 6 us), else by memory: 16384 tokens of 8 heads of 128 (fp16 read, codes written, 109 MB) 31 us, 3.5 TB/s (fp32, 176 MB: 42, 4.2); a
 // unit's loads all go out before the first is looked at, which is 4 us of that.
 #include "cache8.h"
 #include "rope_rows.h"

@@ -43,7 +43,8 @@ __device__ __forceinline__ float weight_far(float s, float scale, float lse) {
 // ---- few rows: the new tokens of a batch ----
 // A wave takes 64 keys and holds them while it goes through the rows, 16 at a time.  Bound by reading K once: everything that
 // does not wait for the page table goes out in front of it, and the keys all at once.  Two tokens of 6 sequences of up to
-// 49159 keys, 8 heads in 8 bits (262 MB): 44 us, 6.0 TB/s (16 keys a wave: 71).
+// 49159 keys, 8 heads in 8 bits (262 MB): 54 us, 4.9 TB/s; with the same inputs again, part of which the last-level cache still
+// holds, 44 (16 keys a wave: 71).
 constexpr int WT_KEYS = 64;              // of a wave
 
 template <class TY, int D, bool E8>
@@ -200,9 +201,13 @@ __global__ __launch_bounds__(256) void k_weights(WeightArgs a) {
 // those of each block of keys in order.
 //
 // A wave holds 64 of the 256 keys in registers and goes through the rows by v_mfma_f32_32x32x16; rows go straight to LDS a tile
-// ahead and are read by all four waves.  Bound by the exponentials: for 32 x 32 scores 256 cycles of products beside 16 times (an
-// addition to the product, an exponential, a sum).  Hence the exponent as one operation, log2(e) in the scale and
-// in the lse that is prepared with the rows, and the next products between the exponentials.
+// ahead and are read by all four waves.  For 32 x 32 scores stand 256 cycles of products beside 16 times (an addition to the product, an
+// exponential, a sum).  Hence the exponent as one operation, log2(e) in the scale and in the lse that is prepared with the
+// rows, and the next products between the exponentials.  Of the SIMDs' cycles the matrix units are busy for 43 % and vector instructions
+// issue in 56 % with one prompt of 16384 tokens (1.13 ms; the power limit lowers the clock to 1.9 GHz), 22 % and 35 % with 23 prompts of 59 to
+// 1458 tokens (88 us, 2.4 GHz): there a run of 14 tiles meets two blocks of keys, each of which begins with nothing in
+// flight, 1.10 times the scores asked for are formed, a fifth of them masked, and waves wait for 41 % of their time.  At d = 128 23 registers and
+// some scalars spill: they are stored and read back around the tiles of a block of keys, not within.
 
 // Inclusive sums over the lanes of a wave; wide: of numbers below 2^45, past 31 bits in two parts.
 __device__ __forceinline__ int64_t weight_scan(int64_t v, bool wide) {
