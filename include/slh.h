@@ -635,9 +635,10 @@ int slh_attend_paged_e4m3(const void *q, int64_t q_st, int64_t q_sh, const void 
  * for rows j < lens[b] (weights of others are left alone).  Queries cu_q[b] <= t < cu_q[b + 1] of q (device, B + 1 entries as for
  * slh_attend; NULL: Tq / B each) are sequence b's; query i of n sees the first lens[b] - n + i + 1 rows.  lse: [Tq][Hq], as
  * slh_attend or slh_attend_paged gave it for the same queries (over all that they saw, a prefix too); a query whose
- * lse is -inf gives nothing.  Scores and lse are fp32, whose rounding leaves a weight with an error of about 2^-22 |lse| of itself where both are
- * large; a key that has all of a query's weight has 1 at any score below fp32's end.  k_cache: pages as slh_kv_append writes them, of dtype (SLH_BF16 or SLH_F16; page_size a power of two up to
- * 65536), or, with k_scale, in 8 bits.  weights: [B][Hkv][max_pages page_size] floats.  Sums are fp32, in an order that
+ * lse is -inf gives nothing.  Scores and lse are fp32, whose rounding leaves a weight with an error of about 2^-22 |lse| of
+ * itself where both are large; a key that has all of a query's weight has 1 at any score below fp32's end.
+ * k_cache: pages as slh_kv_append writes them, of dtype (SLH_BF16 or SLH_F16; page_size a power of two up to 65536),
+ * or, with k_scale, in 8 bits.  weights: [B][Hkv][max_pages page_size] floats.  Sums are fp32, in an order that
  * is the same every call.  lens, page_table, heads, d, scale and strides as for slh_attend_paged.
  * workspace: slh_attend_weights_workspace() bytes, with max_len = max_pages page_size.
  * Limits: as for slh_attend_paged, and B Hkv (max_len / 128 + 1) <= 2^23.

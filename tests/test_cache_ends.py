@@ -191,3 +191,59 @@ def test_weights_of_entries_that_do_not_ascend(block):
             P.slh_attend_weights(q[lo:hi].contiguous(), kc, table[b:b + 1], ints(lens[b:b + 1]), lse[lo:hi].contiguous(), one, cu_q=ints([0, hi - lo]), k_scale=ks)
         # the same positive terms, in another order
         assert bool(((w[b] - one[0]).abs() <= 2 * T * Hq * 2.0 ** -24 * one[0]).all()), b
+
+
+@gpu
+@pytest.mark.parametrize("block", [0, 32])
+@pytest.mark.parametrize("share", [0.02, 0.5])
+def test_weights_of_packed_prompts_with_large_scores_here_and_there(block, share):
+    """Runs of several tiles and blocks of keys, in which some queries' scores are large: 64 runs a head take about seven tiles each."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(block + int(100 * share))
+    d, page, Hkv, Hq, new, lens = 64, 64, 8, 32, [1500, 700, 1100], [1500, 760, 2000]
+    pages = [-(-n // page) for n in lens]
+    x = torch.randn(sum(pages), Hkv, page, d, generator=g, device="cuda")
+    x[..., 0] = 64
+    if block:
+        kc, ks = CP.held(x.cpu(), block)
+        k, kc, ks = CP.values(kc, ks).cuda(), kc.cuda(), ks.cuda()
+    else:
+        kc, ks = x.to(BF), None
+        k = kc.double()
+    table = torch.zeros(3, max(pages), dtype=torch.int32)
+    cu, at = [0], 0
+    for b, n in enumerate(pages):
+        table[b, :n] = torch.arange(at, at + n)
+        at += n
+        cu.append(cu[-1] + new[b])
+    q = torch.randn(cu[-1], Hq, d, generator=g, device="cuda")
+    far = torch.rand(cu[-1], Hq, generator=g, device="cuda") < share
+    q[..., 0] = torch.where(far, 100.0, 0.0)                             # scores of 6400 beside those of 0
+    q = q.to(BF)
+    lse = torch.empty(cu[-1], Hq, device="cuda")
+    wants = []
+    for b, (n, m) in enumerate(zip(new, lens)):
+        kk = k[table[b, :pages[b]].long().cuda()].transpose(1, 2).flatten(0, 1)[:m]
+        hide = torch.arange(m, device="cuda")[None] >= torch.arange(n, device="cuda")[:, None] + m - n + 1
+        want, tol = (torch.zeros(Hkv, m, dtype=torch.float64, device="cuda") for _ in range(2))
+        for h in range(Hq):
+            qq, kh = q[cu[b]:cu[b + 1], h].double(), kk[:, h // 4]
+            s = (qq @ kh.t().contiguous()).masked_fill(hide, -math.inf)
+            ll = torch.logsumexp(s, -1).float()
+            lse[cu[b]:cu[b + 1], h] = ll
+            ll = ll.double()[:, None]
+            p = torch.exp(s - ll)
+            s = s.masked_fill(hide, 0.0)
+            # the error of a weight as in cache_plain.weights; terms below the smallest normal number may be zeros
+            u = 2.0 ** -24
+            e = 2 * d * u * (qq.abs() @ kh.abs().t().contiguous()) + 2 * u * (s.abs() + ll.abs()) + 4 * u * (s - ll).abs() + 4 * u
+            want[h // 4] += p.sum(0)
+            tol[h // 4] += (p * (e + n * 4 * u)).sum(0) + n * 2.0 ** -126
+        wants.append((want, tol))
+    w = torch.zeros(3, Hkv, max(pages) * page, device="cuda")
+    P.slh_attend_weights(q, kc, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), lse, w, cu_q=torch.tensor(cu, dtype=torch.int32).cuda(),
+                         k_scale=ks, scale=1.0)
+    for b, (want, tol) in enumerate(wants):
+        got = w[b, :, :lens[b]].double()
+        assert bool(((got - want).abs() <= tol).all()), (b, float(((got - want).abs() - tol).max()))
+        assert not bool(w[b, :, lens[b]:].any())
